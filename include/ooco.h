@@ -415,6 +415,129 @@ ooco_status ooco_kv_append(ooco_ctx *ctx, const void *k_new /*DEVICE*/, const vo
                            const int32_t *query_start_loc /*DEVICE*/, const int32_t *ctx_lens /*DEVICE*/,
                            int num_seqs, int total_q_tokens, void *stream);
 
+/* ---------------------------------------------------------------------------------------
+ * A step of speculative decoding.  Each sequence has a tree of drafted tokens, its nodes: rows query_start_loc[i] ..
+ * query_start_loc[i+1] - 1 of the step, node 0 (the root) the token that the last step ended with, every other node a
+ * candidate for the token after its parent.  The step of one layer is ooco_rope_append and ooco_attn_tree, with masks and
+ * positions that ooco_tree_masks makes once for all layers; ooco_verify_drafts decides which nodes stay, and
+ * ooco_kv_compact brings their K and V to their places in the caches of all layers.  Node j is token ctx_lens[i] + j of the
+ * cache until then.  None of these calls needs a plan or a host copy of a length, none synchronises or copies: they can be
+ * recorded into a HIP graph, and a graph replays with the lengths that the device arrays then hold.  Calls are made with
+ * the context's device current (-> OOCO_EINVAL).  Sequences of 0 rows, and sequences whose query_start_loc runs outside
+ * [0, total_q_tokens], take no part.
+ *
+ * Masks and positions.  Node t sees node j if j is t or an ancestor of t:
+ *   parents: DEVICE int32 [total_q_tokens], the parent's node number within the sequence, 0 <= parent < t; -1 for the
+ *     root (anything else counts as -1)
+ *   masks: DEVICE uint64 [total_q_tokens][mask_words], written: bit j % 64 of word j / 64
+ *   positions: DEVICE int32 [total_q_tokens], written: ctx_lens[i] + depth of the node; may be NULL
+ * 1 <= mask_words <= 4.  Masks hold the first 64 * mask_words nodes of a sequence; rows behind them get an empty mask and
+ * the position ctx_lens[i].  One kernel. */
+ooco_status ooco_tree_masks(ooco_ctx *ctx, const int32_t *parents /*DEVICE*/, const int32_t *query_start_loc /*DEVICE*/,
+                            const int32_t *ctx_lens /*DEVICE*/, uint64_t *masks /*DEVICE*/, int32_t *positions /*DEVICE or NULL*/,
+                            int mask_words, int num_seqs, int total_q_tokens, void *stream);
+
+/* Rotation frequencies: radians per position of each pair of rotated dims, f_i = base^(-2 i / rotary_dim), 0 <= i <
+ * rotary_dim / 2, stretched for contexts `scale` (s >= 1) times as long as the original_positions that a model was trained on:
+ *   OOCO_ROPE_PLAIN       as they are
+ *   OOCO_ROPE_LINEAR      f_i / s: positions interpolated
+ *   OOCO_ROPE_BASE        base * s^(d / (d - 2)) for base, d = rotary_dim >= 4: the last pair turns s times slower, the first as before
+ *   OOCO_ROPE_WAVELENGTH  by the turns n_i = original_positions * f_i / (2 pi): f_i where n_i > high, f_i / s where n_i < low, between
+ *                         them a mix of weight (n_i - low) / (high - low) of the former
+ *   OOCO_ROPE_RAMP        a mix of f_i and f_i / s that falls linearly over the pairs' numbers, from floor(c(high)) on, where it is
+ *                         all f_i, to ceil(c(low)), c(n) = d ln(original_positions / (2 pi n)) / (2 ln base), both within
+ *                         [0, d - 1]; cosine and sine are then scaled by 0.1 ln s + 1
+ * low and high are used by the last two (low < high).  h_frequencies: HOST double [rotary_dim / 2]; factor: HOST, what cosine
+ * and sine are scaled by (1 but for the last).  Pure HOST function. */
+#define OOCO_ROPE_PLAIN 0
+#define OOCO_ROPE_LINEAR 1
+#define OOCO_ROPE_BASE 2
+#define OOCO_ROPE_WAVELENGTH 3
+#define OOCO_ROPE_RAMP 4
+ooco_status ooco_rope_frequencies(int kind, int rotary_dim, double base, double scale, double original_positions, double low,
+                                  double high, double *h_frequencies /*HOST*/, double *factor /*HOST*/, char *msg /*HOST*/,
+                                  size_t msg_cap);
+
+/* The context's rotation, for ooco_rope_append: the first rotary_dim dims of a head turn in pairs, pair i by the angle
+ * position * h_frequencies[i] (HOST double [rotary_dim / 2], finite): dims (i, i + rotary_dim / 2), or (2 i, 2 i + 1) with
+ * interleaved != 0.  rotary_dim: a positive multiple of 16, at most head_dim (-> OOCO_ESHAPE).  factor scales cosine and sine.
+ * Host work; later calls use it, calls already made keep what they had. */
+ooco_status ooco_rope_set(ooco_ctx *ctx, int rotary_dim, int interleaved, const double *h_frequencies /*HOST*/, double factor);
+
+/* Rotary positions and KV append in one pass over q, k and v: q_out = q rotated; k rotated and v as it is go to the paged
+ * slots that ooco_kv_append writes.  Row query_start_loc[i] + t turns by positions[row], or by ctx_lens[i] + t if positions
+ * is NULL; its slot is that of token ctx_lens[i] + t either way.
+ *   q: DEVICE bf16, row r at q + r * q_stride, [Hq][hd] contiguous there; k_new, v_new likewise, [Hkv][hd] with k_stride and
+ *     v_stride (elements): the rows may lie inside a wider tensor, for instance side by side in one projection's output
+ *   q_out: DEVICE bf16 [total_q_tokens][Hq][hd] contiguous; q itself, if q is contiguous too (q_stride == Hq * hd)
+ *   positions: DEVICE int32 [total_q_tokens] or NULL
+ * All pointers to bf16 values 16-byte aligned, strides multiples of 8 and not below a row (-> OOCO_EINVAL).  Angles are reduced in
+ * 64 bits, rotated in fp32 and rounded once to bf16 (nearest even).  Rows that the cache has no slot for (position beyond the block
+ * table, block id outside [0, num_blocks)) are rotated into q_out and not appended; no other element of the pools changes.
+ * Needs ooco_rope_set before (-> OOCO_EINVAL).  One kernel. */
+ooco_status ooco_rope_append(ooco_ctx *ctx, const void *q /*DEVICE*/, int64_t q_stride, const void *k_new /*DEVICE*/,
+                             int64_t k_stride, const void *v_new /*DEVICE*/, int64_t v_stride, const int32_t *positions /*DEVICE or NULL*/,
+                             void *q_out /*DEVICE*/, void *k_cache /*DEVICE*/, void *v_cache /*DEVICE*/,
+                             const int32_t *block_tables /*DEVICE*/, const int32_t *query_start_loc /*DEVICE*/,
+                             const int32_t *ctx_lens /*DEVICE*/, int num_seqs, int total_q_tokens, void *stream);
+
+/* Attention of the nodes: row t of sequence i sees tokens 0 .. ctx_lens[i] - 1 and node j of the sequence (token
+ * ctx_lens[i] + j, already in the cache) if bit j % 64 of masks[row][j / 64] is set; nodes from 64 * mask_words on are seen by
+ * nobody, and bits behind the sequence's last node mean nothing.  The masks need not come from a tree.
+ *   q, out: DEVICE bf16 [total_q_tokens][Hq][hd], 16-byte aligned; masks: DEVICE uint64 [total_q_tokens][mask_words],
+ *   1 <= mask_words <= 4; k_cache, v_cache, block_tables as for ooco_attn_mixed (no token beyond the block table is seen; ids are
+ *   clamped to the pool).
+ * out = softmax(scale * q K^T) V with fp32 statistics and accumulation, rounded to bf16; a row that sees nothing, or nothing but
+ * scores of -inf, is zero.  A score of NaN or +inf reaches the rows and heads that see it, and no others.  V has to be finite in
+ * every slot of a sequence below ctx_lens[i] + its nodes, also where a row does not see the token.
+ * Any number of sequences and rows.  Partial results lie in the context's workspace (33 KiB per run of head_dim 128; fewer runs where
+ * it is small, OOCO_ENOMEM where it holds none).  Same context, lengths and inputs: the same bits.  Two kernels. */
+ooco_status ooco_attn_tree(ooco_ctx *ctx, const void *q /*DEVICE*/, const void *k_cache /*DEVICE*/, const void *v_cache /*DEVICE*/,
+                           const int32_t *block_tables /*DEVICE*/, const int32_t *query_start_loc /*DEVICE*/,
+                           const int32_t *ctx_lens /*DEVICE*/, const uint64_t *masks /*DEVICE*/, int mask_words, void *out /*DEVICE*/,
+                           int num_seqs, int total_q_tokens, void *stream);
+
+/* Verification of the drafted tokens.  Row r of target_probs is the target model's distribution of the token after node r.
+ * From the root on, the children of a node v are looked at in the order of their numbers: child c with token x is accepted if
+ *   uniforms[c] * q_c(x) * (1 - sum of p_v over the tokens of the siblings refused before) < p_v(x)       (in 64 bits)
+ * with p_v = row v of target_probs -- 0 for a token that a refused sibling had -- and q_c = row c of draft_probs, the
+ * distribution that c's token was drawn from; draft_probs == NULL: q_c(x) = 1, for tokens that were picked.  The walk goes on
+ * from the first accepted child; it ends at a node without one, or after max_path nodes.  One more token is drawn from what is left at
+ * that node v: max(p_v - q_c, 0) for the refused child c, or p_v without the refused children's tokens (all of p_v after max_path
+ * nodes, or if nothing is left): the first token whose running sum exceeds final_uniforms[i] times the whole sum (or, where rounding
+ * leaves none, the last one that has any weight).  Tokens drawn so are distributed as the target's, whatever the draft.
+ *   target_probs, draft_probs: DEVICE, fp32 (bf16_probs == 0) or bf16, rows row_stride >= vocab elements apart, aligned to their
+ *     element; values that are not finite, or negative, have no weight
+ *   tokens: DEVICE int32 [total_q_tokens] (the root's is not looked at; one outside [0, vocab) is never accepted)
+ *   parents: DEVICE int32 [total_q_tokens] as for ooco_tree_masks, or NULL: chains, the parent of node t is t - 1.  Trees with
+ *     draft_probs are refused (OOCO_EINVAL).
+ *   uniforms: DEVICE float [total_q_tokens], final_uniforms: DEVICE float [num_seqs], in [0, 1)
+ *   counts: DEVICE int32 [num_seqs], written: accepted nodes + 1 = tokens that the step yields (0 for a sequence without
+ *     rows).  ctx_lens[i] + counts[i] tokens of the cache are then valid, once ooco_kv_compact has run.
+ *   path: DEVICE int32 [num_seqs][max_path], written: the accepted nodes, then -1
+ *   out_tokens: DEVICE int32 [num_seqs][max_path + 1], written: their tokens and the drawn one, then -1 (the drawn one is -1
+ *     where the target's row has no weight at all)
+ * The first 256 nodes of a sequence take part.  0 <= max_path.  Sums of pieces lie in the context's workspace (OOCO_ENOMEM if it is too
+ * small, or beyond 2^19 sequences).  One kernel. */
+ooco_status ooco_verify_drafts(ooco_ctx *ctx, const void *target_probs /*DEVICE*/, const void *draft_probs /*DEVICE or NULL*/,
+                               int bf16_probs, int vocab, int64_t row_stride, const int32_t *tokens /*DEVICE*/,
+                               const int32_t *parents /*DEVICE or NULL*/, const float *uniforms /*DEVICE*/,
+                               const float *final_uniforms /*DEVICE*/, const int32_t *query_start_loc /*DEVICE*/,
+                               int32_t *counts /*DEVICE*/, int32_t *path /*DEVICE*/, int32_t *out_tokens /*DEVICE*/, int max_path,
+                               int num_seqs, int total_q_tokens, void *stream);
+
+/* The accepted nodes' K and V to the slots behind the cached tokens, in the caches of num_layers layers: token
+ * ctx_lens[i] + path[i][d] becomes token ctx_lens[i] + 1 + d, 0 <= d < counts[i] - 1 (the root is in its place).  Bit-exact; no
+ * other element of the pools changes.
+ *   h_k_caches, h_v_caches: HOST arrays of num_layers DEVICE pools of this context's geometry, pairwise distinct
+ *   path: DEVICE int32 [num_seqs][max_path], rising, counts: DEVICE int32 [num_seqs], as ooco_verify_drafts writes them;
+ *   ctx_lens as in the step, before it is advanced
+ * At most 256 nodes of a path are moved.  A node whose path entry does not exceed its place d + 1 stays, and so does one whose slot or
+ * place lies beyond the block table or in a block outside [0, num_blocks).  One kernel per 112 layers. */
+ooco_status ooco_kv_compact(ooco_ctx *ctx, void *const *h_k_caches /*HOST*/, void *const *h_v_caches /*HOST*/, int num_layers,
+                            const int32_t *block_tables /*DEVICE*/, const int32_t *ctx_lens /*DEVICE*/, const int32_t *path /*DEVICE*/,
+                            const int32_t *counts /*DEVICE*/, int max_path, int num_seqs, void *stream);
+
 /* Roofline latency model of the attention operator (paper Section 3.3: Table 2 gives the operator's
  * FLOPs 4*D_h*S_q*S_kv and bytes 2d*(S_q*D_h + S_kv*D_h*H_kv/H_q) with D_h = H_q*head_dim.  Table 2 as
  * printed shows the head ratio of the KV term as H_q/H_kv; the library uses H_kv/H_q, because the KV

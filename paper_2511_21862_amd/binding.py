@@ -20,7 +20,8 @@ _STATUS_NAMES = {0: "OOCO_OK", -1: "OOCO_EINVAL", -2: "OOCO_ESHAPE", -3: "OOCO_E
 
 EXPORTS = ["ooco_ctx_create", "ooco_ctx_destroy", "ooco_last_error", "ooco_set_option", "ooco_plan",
            "ooco_plan_dry_run", "ooco_plan_info", "ooco_plan_kernels", "ooco_profile_read", "ooco_profile_read_calls", "ooco_trace_read", "ooco_attn_mixed", "ooco_attn_mixed_static", "ooco_kv_block_copy", "ooco_kv_append", "ooco_predict_latency", "ooco_mix_decoding_select",
-           "ooco_migration_preference", "ooco_migration_select", "ooco_eviction_victims"]
+           "ooco_migration_preference", "ooco_migration_select", "ooco_eviction_victims", "ooco_tree_masks", "ooco_rope_frequencies",
+           "ooco_rope_set", "ooco_rope_append", "ooco_attn_tree", "ooco_verify_drafts", "ooco_kv_compact"]
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2511_21862_amd.build` "
@@ -69,6 +70,20 @@ _lib.ooco_kv_block_copy.restype = ctypes.c_int
 _lib.ooco_kv_block_copy.argtypes = [_P] * 7 + [ctypes.c_int64, _P]
 _lib.ooco_kv_append.restype = ctypes.c_int
 _lib.ooco_kv_append.argtypes = [_P] * 8 + [ctypes.c_int, ctypes.c_int, _P]
+_lib.ooco_tree_masks.restype = ctypes.c_int
+_lib.ooco_tree_masks.argtypes = [_P] * 6 + [ctypes.c_int] * 3 + [_P]
+_lib.ooco_rope_frequencies.restype = ctypes.c_int
+_lib.ooco_rope_frequencies.argtypes = [ctypes.c_int] * 2 + [ctypes.c_double] * 5 + [_P, _P, ctypes.c_char_p, ctypes.c_size_t]
+_lib.ooco_rope_set.restype = ctypes.c_int
+_lib.ooco_rope_set.argtypes = [_P, ctypes.c_int, ctypes.c_int, _P, ctypes.c_double]
+_lib.ooco_rope_append.restype = ctypes.c_int
+_lib.ooco_rope_append.argtypes = [_P] + [_P, ctypes.c_int64] * 3 + [_P] * 7 + [ctypes.c_int, ctypes.c_int, _P]
+_lib.ooco_attn_tree.restype = ctypes.c_int
+_lib.ooco_attn_tree.argtypes = [_P] * 8 + [ctypes.c_int, _P] + [ctypes.c_int] * 2 + [_P]
+_lib.ooco_verify_drafts.restype = ctypes.c_int
+_lib.ooco_verify_drafts.argtypes = ([_P] * 3 + [ctypes.c_int, ctypes.c_int, ctypes.c_int64] + [_P] * 8 + [ctypes.c_int] * 3 + [_P])
+_lib.ooco_kv_compact.restype = ctypes.c_int
+_lib.ooco_kv_compact.argtypes = [_P] * 3 + [ctypes.c_int] + [_P] * 4 + [ctypes.c_int, ctypes.c_int, _P]
 
 
 
@@ -319,6 +334,86 @@ def ooco_kv_append(ctx, k_new, v_new, k_cache, v_cache, block_tables, query_star
                                     _stream_handle(stream)))
 
 
+def ooco_tree_masks(ctx, parents, query_start_loc, ctx_lens, masks, positions, mask_words, num_seqs, total_q_tokens, stream=None) -> None:
+    _check(ctx, _lib.ooco_tree_masks(ctx, _dev(parents), _dev(query_start_loc), _dev(ctx_lens), _dev(masks), _dev(positions), mask_words,
+                                     num_seqs, total_q_tokens, _stream_handle(stream)))
+
+
+ROPE_KINDS = ("plain", "linear", "base", "wavelength", "ramp")
+
+
+def ooco_rope_frequencies(kind, rotary_dim, base=10000.0, scale=1.0, original_positions=0.0, low=1.0, high=2.0) -> dict:
+    """kind: one of ROPE_KINDS.  Returns dict(frequencies=float64 [rotary_dim / 2], factor=scale of cosine and sine)."""
+    if kind not in ROPE_KINDS:
+        raise ValueError(f"kind: one of {ROPE_KINDS}")
+    f = np.zeros(max(1, rotary_dim // 2), dtype=np.float64)
+    factor = ctypes.c_double()
+    msg = ctypes.create_string_buffer(256)
+    st = _lib.ooco_rope_frequencies(ROPE_KINDS.index(kind), rotary_dim, float(base), float(scale), float(original_positions), float(low),
+                                    float(high), f.ctypes.data, ctypes.addressof(factor), msg, 256)
+    if st != OOCO_OK:
+        raise OocoError(st, msg.value.decode())
+    return dict(frequencies=f, factor=factor.value)
+
+
+def ooco_rope_set(ctx, rotary_dim, interleaved, frequencies, factor=1.0) -> None:
+    f = None if frequencies is None else np.ascontiguousarray(frequencies, dtype=np.float64)
+    if f is not None and f.size != rotary_dim // 2:
+        raise ValueError(f"{f.size} frequencies for rotary_dim {rotary_dim}")
+    _check(ctx, _lib.ooco_rope_set(ctx, rotary_dim, int(bool(interleaved)), 0 if f is None else f.ctypes.data, float(factor)))
+
+
+def _rows(t):
+    """Device pointer and row stride (elements) of a tensor whose rows are contiguous, [rows][heads][head_dim] or [rows][values]."""
+    if t is None:
+        return 0, 0
+    inner = 1
+    for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        if size != 1 and stride != inner:
+            raise ValueError("the rows of tensors passed to ooco_rope_append must be contiguous")
+        inner *= size
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), inner)
+
+
+def ooco_rope_append(ctx, q, k_new, v_new, positions, q_out, k_cache, v_cache, block_tables, query_start_loc, ctx_lens, num_seqs,
+                     total_q_tokens, stream=None) -> None:
+    """q, k_new and v_new may be views of a wider tensor (rows contiguous, any distance between them)."""
+    _check(ctx, _lib.ooco_rope_append(ctx, *_rows(q), *_rows(k_new), *_rows(v_new), _dev(positions), _dev(q_out), _dev(k_cache),
+                                      _dev(v_cache), _dev(block_tables), _dev(query_start_loc), _dev(ctx_lens), num_seqs,
+                                      total_q_tokens, _stream_handle(stream)))
+
+
+def ooco_attn_tree(ctx, q, k_cache, v_cache, block_tables, query_start_loc, ctx_lens, masks, mask_words, out, num_seqs, total_q_tokens,
+                   stream=None) -> None:
+    _check(ctx, _lib.ooco_attn_tree(ctx, _dev(q), _dev(k_cache), _dev(v_cache), _dev(block_tables), _dev(query_start_loc),
+                                    _dev(ctx_lens), _dev(masks), mask_words, _dev(out), num_seqs, total_q_tokens,
+                                    _stream_handle(stream)))
+
+
+def ooco_verify_drafts(ctx, target_probs, draft_probs, tokens, parents, uniforms, final_uniforms, query_start_loc, counts, path,
+                       out_tokens, max_path, num_seqs, total_q_tokens, stream=None) -> None:
+    """target_probs, draft_probs: float32 or bfloat16 [rows][vocab], rows contiguous, equally far apart in both."""
+    if target_probs.dtype not in (torch.float32, torch.bfloat16) or (draft_probs is not None and draft_probs.dtype != target_probs.dtype):
+        raise ValueError("probabilities are float32 or bfloat16, the draft's as the target's")
+    if target_probs.stride(1) != 1 or (draft_probs is not None and draft_probs.stride() != target_probs.stride()):
+        raise ValueError("rows of probabilities must be contiguous, and as far apart in the draft's as in the target's")
+    vocab = target_probs.shape[1]
+    _check(ctx, _lib.ooco_verify_drafts(ctx, target_probs.data_ptr(), 0 if draft_probs is None else draft_probs.data_ptr(),
+                                        int(target_probs.dtype == torch.bfloat16), vocab, max(target_probs.stride(0), vocab), _dev(tokens),
+                                        _dev(parents), _dev(uniforms), _dev(final_uniforms), _dev(query_start_loc), _dev(counts),
+                                        _dev(path), _dev(out_tokens), max_path, num_seqs, total_q_tokens, _stream_handle(stream)))
+
+
+def ooco_kv_compact(ctx, k_caches, v_caches, block_tables, ctx_lens, path, counts, max_path, num_seqs, stream=None) -> None:
+    """k_caches, v_caches: the pools of all layers, one tensor each."""
+    n = len(k_caches)
+    if len(v_caches) != n:
+        raise ValueError(f"{n} pools of K and {len(v_caches)} of V")
+    ks, vs = (_P * n)(*[_dev(t) for t in k_caches]), (_P * n)(*[_dev(t) for t in v_caches])
+    _check(ctx, _lib.ooco_kv_compact(ctx, ks, vs, n, _dev(block_tables), _dev(ctx_lens), _dev(path), _dev(counts), max_path, num_seqs,
+                                     _stream_handle(stream)))
+
+
 def ooco_predict_latency(params, num_q_heads, num_kv_heads, head_dim, h_query_start_loc, h_ctx_lens,
                          bytes_per_value=2, causal_flops=False) -> dict:
     """params: dict or ModelParams.  Returns the model's outputs by name (argument marshalling only)."""
@@ -485,3 +580,27 @@ class Context:
         if st is not NotImplemented:
             return _check(self.h, st)
         ooco_kv_block_copy(self.h, k_src, v_src, k_dst, v_dst, src_ids, dst_ids, int(src_ids.shape[0]), stream)
+
+    def tree_masks(self, parents, query_start_loc, ctx_lens, masks, positions=None, stream=None):
+        ooco_tree_masks(self.h, parents, query_start_loc, ctx_lens, masks, positions, int(masks.shape[1]), int(ctx_lens.shape[0]),
+                        int(parents.shape[0]), stream)
+
+    def rope_set(self, frequencies, interleaved=False, factor=1.0):
+        ooco_rope_set(self.h, 2 * len(frequencies), interleaved, frequencies, factor)
+
+    def rope_append(self, q, k_new, v_new, q_out, k_cache, v_cache, block_tables, query_start_loc, ctx_lens, positions=None, stream=None):
+        ooco_rope_append(self.h, q, k_new, v_new, positions, q_out, k_cache, v_cache, block_tables, query_start_loc, ctx_lens,
+                         int(ctx_lens.shape[0]), int(q.shape[0]), stream)
+
+    def attn_tree(self, q, k_cache, v_cache, block_tables, query_start_loc, ctx_lens, masks, out, stream=None):
+        ooco_attn_tree(self.h, q, k_cache, v_cache, block_tables, query_start_loc, ctx_lens, masks, int(masks.shape[1]), out,
+                       int(ctx_lens.shape[0]), int(q.shape[0]), stream)
+
+    def verify_drafts(self, target_probs, tokens, uniforms, final_uniforms, query_start_loc, counts, path, out_tokens, draft_probs=None,
+                      parents=None, stream=None):
+        ooco_verify_drafts(self.h, target_probs, draft_probs, tokens, parents, uniforms, final_uniforms, query_start_loc, counts, path,
+                           out_tokens, int(path.shape[1]), int(counts.shape[0]), int(tokens.shape[0]), stream)
+
+    def kv_compact(self, k_caches, v_caches, block_tables, ctx_lens, path, counts, stream=None):
+        ooco_kv_compact(self.h, k_caches, v_caches, block_tables, ctx_lens, path, counts, int(path.shape[1]), int(ctx_lens.shape[0]),
+                        stream)

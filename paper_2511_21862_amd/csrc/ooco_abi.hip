@@ -1,6 +1,7 @@
 // Host side of libooco: context, argument validation, the work-list planner and the C ABI.
 #include "../../include/ooco.h"
 #include "ooco_internal.h"
+#include "ooco_spec.h"
 
 #include <algorithm>
 #include <cmath>
@@ -1029,6 +1030,12 @@ struct ooco_ctx {
     bool plan_dirty = false;
     bool plan_one_shot = false;   // planned inside ooco_attn_mixed from device lengths
     bool plan_made = false;       // ctx->plan holds the numbers of the last plan made (current or used up)
+    // rotation of ooco_rope_append (pairs == 0: not set)
+    int rope_pairs = 0;
+    bool rope_interleaved = false;
+    float rope_factor = 1.f;
+    double rope_turns[kMaxRotaryPairs] = {};
+
     int64_t opt_plan_persistent = 0;   // an explicit plan serves every following call of the same shape
 
     // options
@@ -2021,6 +2028,232 @@ ooco_status ooco_kv_append(ooco_ctx *ctx, const void *k_new, const void *v_new, 
                                     total_q_tokens, ctx->Hkv, ctx->hd, ctx->max_blocks_per_seq, ctx->num_blocks,
                                     (int)ctx->opt_append_parts, ctx->num_cus, reinterpret_cast<hipStream_t>(stream));
     if (e != hipSuccess) return fail(ctx, OOCO_EHIP, "ooco_kv_append: kernel launch: %s", hipGetErrorString(e));
+    return OOCO_OK;
+}
+
+// ---- the speculative decoding step
+
+// What the calls below have in common: sizes, the device, nothing to do.  true: go on.
+static bool step_call(ooco_ctx *ctx, const char *name, int num_seqs, int total_q_tokens, ooco_status &st)
+{
+    st = OOCO_OK;
+    if (num_seqs < 0 || total_q_tokens < 0) {
+        st = fail(ctx, OOCO_EINVAL, "%s: num_seqs=%d total_q_tokens=%d", name, num_seqs, total_q_tokens);
+        return false;
+    }
+    if (num_seqs == 0 || total_q_tokens == 0) return false;
+    int device = 0;
+    const hipError_t e = hipGetDevice(&device);
+    if (e != hipSuccess)
+        st = fail(ctx, OOCO_EHIP, "%s: %s", name, hipGetErrorString(e));
+    else if (device != ctx->device)
+        st = fail(ctx, OOCO_EINVAL, "%s: the context belongs to device %d, the current device is %d", name, ctx->device, device);
+    return st == OOCO_OK;
+}
+static bool aligned(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+ooco_status ooco_tree_masks(ooco_ctx *ctx, const int32_t *parents, const int32_t *query_start_loc, const int32_t *ctx_lens, uint64_t *masks,
+                            int32_t *positions, int mask_words, int num_seqs, int total_q_tokens, void *stream)
+{
+    if (!ctx) return OOCO_EINVAL;
+    if (mask_words < 1 || mask_words > kMaxMaskWords)
+        return fail(ctx, OOCO_ESHAPE, "ooco_tree_masks: mask_words=%d (1 .. %d)", mask_words, kMaxMaskWords);
+    ooco_status st;
+    if (!step_call(ctx, "ooco_tree_masks", num_seqs, total_q_tokens, st)) return st;
+    if (!parents || !query_start_loc || !ctx_lens || !masks) return fail(ctx, OOCO_EINVAL, "ooco_tree_masks: NULL pointer argument");
+    if (!aligned(masks, 8)) return fail(ctx, OOCO_EINVAL, "ooco_tree_masks: masks must be 8-byte aligned");
+    const hipError_t e = launch_tree_masks(parents, query_start_loc, ctx_lens, masks, positions, mask_words, num_seqs, total_q_tokens,
+                                           reinterpret_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return fail(ctx, OOCO_EHIP, "ooco_tree_masks: kernel launch: %s", hipGetErrorString(e));
+    return OOCO_OK;
+}
+
+ooco_status ooco_rope_set(ooco_ctx *ctx, int rotary_dim, int interleaved, const double *h_frequencies, double factor)
+{
+    if (!ctx) return OOCO_EINVAL;
+    if (!h_frequencies) return fail(ctx, OOCO_EINVAL, "ooco_rope_set: NULL pointer argument");
+    if (rotary_dim <= 0 || rotary_dim % 16 || rotary_dim > ctx->hd)
+        return fail(ctx, OOCO_ESHAPE, "ooco_rope_set: rotary_dim=%d must be a positive multiple of 16, at most head_dim=%d", rotary_dim, ctx->hd);
+    if (!std::isfinite(factor)) return fail(ctx, OOCO_EINVAL, "ooco_rope_set: factor is not finite");
+    for (int i = 0; i < rotary_dim / 2; ++i)
+        if (!std::isfinite(h_frequencies[i])) return fail(ctx, OOCO_EINVAL, "ooco_rope_set: frequency %d is not finite", i);
+    for (int i = 0; i < rotary_dim / 2; ++i) ctx->rope_turns[i] = h_frequencies[i] / 6.283185307179586476925287;
+    ctx->rope_pairs = rotary_dim / 2;
+    ctx->rope_interleaved = interleaved != 0;
+    ctx->rope_factor = (float)factor;
+    return OOCO_OK;
+}
+
+ooco_status ooco_rope_append(ooco_ctx *ctx, const void *q, int64_t q_stride, const void *k_new, int64_t k_stride, const void *v_new,
+                             int64_t v_stride, const int32_t *positions, void *q_out, void *k_cache, void *v_cache,
+                             const int32_t *block_tables, const int32_t *query_start_loc, const int32_t *ctx_lens, int num_seqs,
+                             int total_q_tokens, void *stream)
+{
+    if (!ctx) return OOCO_EINVAL;
+    if (!ctx->rope_pairs) return fail(ctx, OOCO_EINVAL, "ooco_rope_append: ooco_rope_set has not been called on this context");
+    ooco_status st;
+    if (!step_call(ctx, "ooco_rope_append", num_seqs, total_q_tokens, st)) return st;
+    if (!q || !k_new || !v_new || !q_out || !k_cache || !v_cache || !block_tables || !query_start_loc || !ctx_lens)
+        return fail(ctx, OOCO_EINVAL, "ooco_rope_append: NULL pointer argument");
+    const int64_t q_row = (int64_t)ctx->Hq * ctx->hd, k_row = (int64_t)ctx->Hkv * ctx->hd;
+    if (q_stride < q_row || k_stride < k_row || v_stride < k_row || (q_stride | k_stride | v_stride) % 8)
+        return fail(ctx, OOCO_EINVAL, "ooco_rope_append: strides %lld, %lld, %lld must be multiples of 8, at least %lld, %lld, %lld", (long long)q_stride,
+                    (long long)k_stride, (long long)v_stride, (long long)q_row, (long long)k_row, (long long)k_row);
+    for (const void *x : {q, k_new, v_new, (const void *)q_out, (const void *)k_cache, (const void *)v_cache})
+        if (!aligned(x, 16)) return fail(ctx, OOCO_EINVAL, "ooco_rope_append: bf16 tensors must be 16-byte aligned");
+    if (q == q_out && q_stride != q_row) return fail(ctx, OOCO_EINVAL, "ooco_rope_append: q_out is q, whose rows are %lld elements apart", (long long)q_stride);
+    if (((int64_t)total_q_tokens / kBlockSize + 2 * (int64_t)num_seqs + 1) * (ctx->Hq + 2 * ctx->Hkv) > INT32_MAX)
+        return fail(ctx, OOCO_ESHAPE, "ooco_rope_append: %d sequences of %d rows are too many for one call", num_seqs, total_q_tokens);
+    RopeArgs a = {};
+    a.q = static_cast<const uint16_t *>(q);
+    a.k_new = static_cast<const uint16_t *>(k_new);
+    a.v_new = static_cast<const uint16_t *>(v_new);
+    a.q_out = static_cast<uint16_t *>(q_out);
+    a.k_cache = static_cast<uint16_t *>(k_cache);
+    a.v_cache = static_cast<uint16_t *>(v_cache);
+    a.positions = positions;
+    a.block_tables = block_tables;
+    a.query_start_loc = query_start_loc;
+    a.ctx_lens = ctx_lens;
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.num_blocks = ctx->num_blocks;
+    a.Hq = ctx->Hq;
+    a.Hkv = ctx->Hkv;
+    a.hd = ctx->hd;
+    a.max_blocks_per_seq = ctx->max_blocks_per_seq;
+    a.num_seqs = num_seqs;
+    a.total_q = total_q_tokens;
+    a.pairs = ctx->rope_pairs;
+    a.factor = ctx->rope_factor;
+    memcpy(a.turns, ctx->rope_turns, sizeof a.turns);
+    const hipError_t e = launch_rope_append(a, ctx->rope_interleaved, ctx->num_cus, reinterpret_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return fail(ctx, OOCO_EHIP, "ooco_rope_append: kernel launch: %s", hipGetErrorString(e));
+    return OOCO_OK;
+}
+
+ooco_status ooco_attn_tree(ooco_ctx *ctx, const void *q, const void *k_cache, const void *v_cache, const int32_t *block_tables,
+                           const int32_t *query_start_loc, const int32_t *ctx_lens, const uint64_t *masks, int mask_words, void *out,
+                           int num_seqs, int total_q_tokens, void *stream)
+{
+    if (!ctx) return OOCO_EINVAL;
+    if (mask_words < 1 || mask_words > kMaxMaskWords)
+        return fail(ctx, OOCO_ESHAPE, "ooco_attn_tree: mask_words=%d (1 .. %d)", mask_words, kMaxMaskWords);
+    ooco_status st;
+    if (!step_call(ctx, "ooco_attn_tree", num_seqs, total_q_tokens, st)) return st;
+    if (!q || !k_cache || !v_cache || !block_tables || !query_start_loc || !ctx_lens || !masks || !out)
+        return fail(ctx, OOCO_EINVAL, "ooco_attn_tree: NULL pointer argument");
+    for (const void *x : {q, k_cache, v_cache, (const void *)out})
+        if (!aligned(x, 16)) return fail(ctx, OOCO_EINVAL, "ooco_attn_tree: bf16 tensors must be 16-byte aligned");
+    if (!aligned(masks, 8)) return fail(ctx, OOCO_EINVAL, "ooco_attn_tree: masks must be 8-byte aligned");
+    TreeArgs a = {};
+    a.runs_log2 = tree_runs_log2(ctx->hd, ctx->num_cus, ctx->ws_bytes);
+    if (a.runs_log2 < 0) return fail(ctx, OOCO_ENOMEM, "ooco_attn_tree: the workspace (%zu bytes) holds no partial result", ctx->ws_bytes);
+    a.q = static_cast<const uint16_t *>(q);
+    a.k_cache = static_cast<const uint16_t *>(k_cache);
+    a.v_cache = static_cast<const uint16_t *>(v_cache);
+    a.block_tables = block_tables;
+    a.query_start_loc = query_start_loc;
+    a.ctx_lens = ctx_lens;
+    a.masks = masks;
+    a.out = static_cast<uint16_t *>(out);
+    a.num_blocks = ctx->num_blocks;
+    a.Hq = ctx->Hq;
+    a.Hkv = ctx->Hkv;
+    a.g = ctx->g;
+    a.hd = ctx->hd;
+    a.max_blocks_per_seq = ctx->max_blocks_per_seq;
+    a.num_seqs = num_seqs;
+    a.total_q = total_q_tokens;
+    a.words = mask_words;
+    a.scale_log2e = ctx->scale * 1.4426950408889634f;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    ctx->note_stream(s);
+    const hipError_t e = launch_attn_tree(a, ctx->ws, s);
+    if (e != hipSuccess) return fail(ctx, OOCO_EHIP, "ooco_attn_tree: kernel launch: %s", hipGetErrorString(e));
+    return OOCO_OK;
+}
+
+ooco_status ooco_verify_drafts(ooco_ctx *ctx, const void *target_probs, const void *draft_probs, int bf16_probs, int vocab, int64_t row_stride,
+                               const int32_t *tokens, const int32_t *parents, const float *uniforms, const float *final_uniforms,
+                               const int32_t *query_start_loc, int32_t *counts, int32_t *path, int32_t *out_tokens, int max_path,
+                               int num_seqs, int total_q_tokens, void *stream)
+{
+    if (!ctx) return OOCO_EINVAL;
+    if (vocab <= 0 || row_stride < vocab || max_path < 0)
+        return fail(ctx, OOCO_EINVAL, "ooco_verify_drafts: vocab=%d row_stride=%lld max_path=%d", vocab, (long long)row_stride, max_path);
+    if (parents && draft_probs) return fail(ctx, OOCO_EINVAL, "ooco_verify_drafts: draft_probs are for chains (parents == NULL)");
+    ooco_status st;
+    if (!step_call(ctx, "ooco_verify_drafts", num_seqs, total_q_tokens, st)) return st;
+    if (!target_probs || !tokens || !uniforms || !final_uniforms || !query_start_loc || !counts || (max_path && !path) || !out_tokens)
+        return fail(ctx, OOCO_EINVAL, "ooco_verify_drafts: NULL pointer argument");
+    if (!aligned(target_probs, bf16_probs ? 2 : 4) || !aligned(draft_probs, bf16_probs ? 2 : 4))
+        return fail(ctx, OOCO_EINVAL, "ooco_verify_drafts: probabilities must be aligned to their element");
+    if ((size_t)num_seqs > kCounterInts / 2) return fail(ctx, OOCO_ENOMEM, "ooco_verify_drafts: %d sequences (at most %zu)", num_seqs, kCounterInts / 2);
+    VerifyArgs a = {};
+    a.target = target_probs;
+    a.draft = draft_probs;
+    a.tokens = tokens;
+    a.parents = parents;
+    a.uniforms = uniforms;
+    a.final_uniforms = final_uniforms;
+    a.query_start_loc = query_start_loc;
+    a.counts = counts;
+    a.path = path;
+    a.out_tokens = out_tokens;
+    a.sums = static_cast<double *>(ctx->ws);
+    a.arrivals = ctx->counters;
+    a.stride = row_stride;
+    a.vocab = vocab;
+    a.max_path = max_path;
+    a.num_seqs = num_seqs;
+    a.total_q = total_q_tokens;
+    verify_chunks(a, ctx->num_cus);
+    if (verify_workspace(a) > ctx->ws_bytes)
+        return fail(ctx, OOCO_ENOMEM, "ooco_verify_drafts: the sums take %zu bytes of workspace, there are %zu", verify_workspace(a), ctx->ws_bytes);
+    if ((int64_t)num_seqs * a.chunks > INT32_MAX) return fail(ctx, OOCO_ENOMEM, "ooco_verify_drafts: %d sequences of %d pieces", num_seqs, a.chunks);
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    ctx->note_stream(s);
+    const hipError_t e = launch_verify(a, bf16_probs != 0, s);
+    if (e != hipSuccess) return fail(ctx, OOCO_EHIP, "ooco_verify_drafts: kernel launch: %s", hipGetErrorString(e));
+    return OOCO_OK;
+}
+
+ooco_status ooco_kv_compact(ooco_ctx *ctx, void *const *h_k_caches, void *const *h_v_caches, int num_layers, const int32_t *block_tables,
+                            const int32_t *ctx_lens, const int32_t *path, const int32_t *counts, int max_path, int num_seqs, void *stream)
+{
+    if (!ctx) return OOCO_EINVAL;
+    if (num_layers < 0 || max_path < 0) return fail(ctx, OOCO_EINVAL, "ooco_kv_compact: num_layers=%d max_path=%d", num_layers, max_path);
+    ooco_status st;
+    if (!step_call(ctx, "ooco_kv_compact", num_seqs, 1, st)) return st;
+    if (num_layers == 0 || max_path == 0) return OOCO_OK;
+    if (!h_k_caches || !h_v_caches || !block_tables || !ctx_lens || !path || !counts)
+        return fail(ctx, OOCO_EINVAL, "ooco_kv_compact: NULL pointer argument");
+    for (int i = 0; i < num_layers; ++i) {
+        if (!h_k_caches[i] || !h_v_caches[i]) return fail(ctx, OOCO_EINVAL, "ooco_kv_compact: the pool of layer %d is NULL", i);
+        if (!aligned(h_k_caches[i], 16) || !aligned(h_v_caches[i], 16))
+            return fail(ctx, OOCO_EINVAL, "ooco_kv_compact: the pools of layer %d must be 16-byte aligned", i);
+    }
+    CompactArgs a = {};
+    a.block_tables = block_tables;
+    a.ctx_lens = ctx_lens;
+    a.path = path;
+    a.counts = counts;
+    a.num_blocks = ctx->num_blocks;
+    a.Hkv = ctx->Hkv;
+    a.hd = ctx->hd;
+    a.max_blocks_per_seq = ctx->max_blocks_per_seq;
+    a.max_path = max_path;
+    for (int first = 0; first < num_layers; first += kCompactLayers) {
+        const int layers = std::min(kCompactLayers, num_layers - first);
+        for (int i = 0; i < layers; ++i) {
+            a.k[i] = static_cast<uint16_t *>(h_k_caches[first + i]);
+            a.v[i] = static_cast<uint16_t *>(h_v_caches[first + i]);
+        }
+        const hipError_t e = launch_kv_compact(a, layers, num_seqs, reinterpret_cast<hipStream_t>(stream));
+        if (e != hipSuccess) return fail(ctx, OOCO_EHIP, "ooco_kv_compact: kernel launch: %s", hipGetErrorString(e));
+    }
     return OOCO_OK;
 }
 

@@ -5,6 +5,7 @@
 #include "ooco.h"
 
 #include <algorithm>
+#include <cmath>
 #include <cstdio>
 #include <cstdlib>
 #include <numeric>
@@ -317,5 +318,45 @@ extern "C" ooco_status ooco_eviction_victims(int num_offline, const int32_t *h_o
     }
     *num_victims = n;
     if (enough) *enough = ok ? 1 : 0;
+    return OOCO_OK;
+}
+
+extern "C" ooco_status ooco_rope_frequencies(int kind, int rotary_dim, double base, double scale, double original_positions, double low,
+                                             double high, double *h_frequencies, double *factor, char *msg, size_t msg_cap)
+{
+    auto bad = [&](ooco_status code, const char *text) {
+        if (msg && msg_cap) snprintf(msg, msg_cap, "ooco_rope_frequencies: %s", text);
+        return code;
+    };
+    if (msg && msg_cap) msg[0] = 0;
+    if (!h_frequencies || !factor) return bad(OOCO_EINVAL, "NULL output");
+    if (rotary_dim <= 0 || rotary_dim % 2) return bad(OOCO_ESHAPE, "rotary_dim must be positive and even");
+    if (kind < OOCO_ROPE_PLAIN || kind > OOCO_ROPE_RAMP) return bad(OOCO_EINVAL, "unknown kind");
+    if (!(base > 1) || !std::isfinite(base)) return bad(OOCO_EINVAL, "base must be above 1");
+    if (kind != OOCO_ROPE_PLAIN && (!(scale >= 1) || !std::isfinite(scale))) return bad(OOCO_EINVAL, "scale must be at least 1");
+    if (kind == OOCO_ROPE_BASE && rotary_dim < 4) return bad(OOCO_ESHAPE, "a stretched base needs rotary_dim of at least 4");
+    const bool banded = kind == OOCO_ROPE_WAVELENGTH || kind == OOCO_ROPE_RAMP;
+    if (banded && (!(original_positions > 0) || !std::isfinite(original_positions) || !(low > 0) || !(low < high) || !std::isfinite(high)))
+        return bad(OOCO_EINVAL, "original_positions must be positive and 0 < low < high");
+    const double d = rotary_dim, two_pi = 6.283185307179586476925287;
+    *factor = 1.0;
+    double first = 0, last = 0;   // OOCO_ROPE_RAMP: the pairs between which the mix falls
+    if (kind == OOCO_ROPE_BASE) base *= std::pow(scale, d / (d - 2));
+    if (kind == OOCO_ROPE_RAMP) {
+        auto pair_of = [&](double turns) { return d * std::log(original_positions / (two_pi * turns)) / (2 * std::log(base)); };
+        first = std::min(std::max(std::floor(pair_of(high)), 0.0), d - 1);
+        last = std::min(std::max(std::ceil(pair_of(low)), 0.0), d - 1);
+        if (last <= first) last = first + 1e-3;   // (a step)
+        *factor = 0.1 * std::log(scale) + 1.0;
+    }
+    for (int i = 0; i < rotary_dim / 2; ++i) {
+        const double f = std::pow(base, -2.0 * i / d);
+        double keep = 1.0;        // weight of f against f / scale
+        if (kind == OOCO_ROPE_LINEAR) keep = 0.0;
+        if (kind == OOCO_ROPE_WAVELENGTH) keep = std::min(std::max((original_positions * f / two_pi - low) / (high - low), 0.0), 1.0);
+        if (kind == OOCO_ROPE_RAMP) keep = 1.0 - std::min(std::max((i - first) / (last - first), 0.0), 1.0);
+        const bool scaled = kind == OOCO_ROPE_LINEAR || banded;
+        h_frequencies[i] = scaled ? keep * f + (1.0 - keep) * (f / scale) : f;
+    }
     return OOCO_OK;
 }

@@ -1,0 +1,96 @@
+// Launchers of the operators of a speculative decoding step (ooco_tree.hip, ooco_spec.hip).  Not part of the public ABI.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace ooco {
+
+constexpr int kMaxMaskWords = 4;   // 64-bit words of a node's mask
+
+// ---- attention of the nodes (ooco_tree.hip)
+struct TreeArgs {
+    const uint16_t *q;
+    const uint16_t *k_cache;
+    const uint16_t *v_cache;
+    const int32_t *block_tables;
+    const int32_t *query_start_loc;
+    const int32_t *ctx_lens;
+    const uint64_t *masks;      // [total_q][words]
+    uint16_t *out;
+    int32_t *merges;            // [runs][kMergeInts]: what the merge kernel has to do at the beginning of each run
+    float *part_acc;            // [2 * runs][columns of a tile][hd]  un-normalised partial outputs
+    float *part_ml;             // [2 * runs][columns of a tile][2]   (running maximum in log2 units, sum)
+    int64_t num_blocks;
+    int32_t Hq, Hkv, g, hd;
+    int32_t max_blocks_per_seq;
+    int32_t num_seqs, total_q, words;
+    int32_t runs_log2;          // runs of the line: 1 << runs_log2 workgroups
+    float scale_log2e;          // softmax scale * log2(e)
+};
+// Runs (a power of two) that a workspace of ws_bytes allows on num_cus compute units, as their logarithm; < 0: none.
+int tree_runs_log2(int hd, int num_cus, size_t ws_bytes);
+// a.runs_log2 runs; the workspace pointers are set from ws.
+hipError_t launch_attn_tree(TreeArgs &a, void *ws, hipStream_t s);
+
+// ---- masks and positions
+hipError_t launch_tree_masks(const int32_t *parents, const int32_t *query_start_loc, const int32_t *ctx_lens, uint64_t *masks,
+                             int32_t *positions, int words, int num_seqs, int total_q, hipStream_t s);
+
+// ---- rotary positions and append
+constexpr int kMaxRotaryPairs = 64;
+struct RopeArgs {
+    const uint16_t *q, *k_new, *v_new;   // rows q_stride, k_stride, v_stride elements apart
+    uint16_t *q_out, *k_cache, *v_cache;
+    const int32_t *positions;            // NULL: the place in the cache
+    const int32_t *block_tables;
+    const int32_t *query_start_loc;
+    const int32_t *ctx_lens;
+    int64_t q_stride, k_stride, v_stride;
+    int64_t num_blocks;
+    int32_t Hq, Hkv, hd;
+    int32_t max_blocks_per_seq;
+    int32_t num_seqs, total_q;
+    int32_t pairs;                       // rotated pairs per head
+    int32_t parts;                       // workgroups per (sequence, KV block)
+    float factor;                        // of cosine and sine
+    double turns[kMaxRotaryPairs];       // turns per position of each pair
+};
+hipError_t launch_rope_append(RopeArgs &a, bool interleaved, int num_cus, hipStream_t s);
+
+// ---- verification
+struct VerifyArgs {
+    const void *target, *draft;          // probabilities, rows `stride` elements apart; draft may be NULL
+    const int32_t *tokens;
+    const int32_t *parents;              // NULL: chains
+    const float *uniforms;               // [total_q]
+    const float *final_uniforms;         // [num_seqs]
+    const int32_t *query_start_loc;
+    int32_t *counts, *path, *out_tokens;
+    double *sums;                        // [num_seqs][chunks][2]
+    int32_t *arrivals;                   // [num_seqs], zero between calls
+    int64_t stride;
+    int32_t vocab, max_path;
+    int32_t num_seqs, total_q;
+    int32_t chunk, chunks;               // elements of a row that a workgroup sums, and such pieces of a row
+};
+constexpr int kMaxVerifyNodes = 256;
+size_t verify_workspace(const VerifyArgs &a);
+void verify_chunks(VerifyArgs &a, int num_cus);
+hipError_t launch_verify(const VerifyArgs &a, bool bf16, hipStream_t s);
+
+// ---- accepted nodes to their places
+constexpr int kCompactLayers = 112;      // layers per launch (their pointers travel in the kernel arguments)
+struct CompactArgs {
+    uint16_t *k[kCompactLayers], *v[kCompactLayers];
+    const int32_t *block_tables;
+    const int32_t *ctx_lens;
+    const int32_t *path;
+    const int32_t *counts;
+    int64_t num_blocks;
+    int32_t Hkv, hd, max_blocks_per_seq, max_path;
+};
+hipError_t launch_kv_compact(const CompactArgs &a, int layers, int num_seqs, hipStream_t s);
+
+}  // namespace ooco

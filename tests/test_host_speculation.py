@@ -1,0 +1,111 @@
+"""Host side of the speculative decoding step: rotation frequencies against their formulas, refusals that need no GPU, and the
+oracle of the step's operators against mathematics."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import speculation as S
+from paper_2511_21862_amd import binding as B
+
+KINDS = [("plain", {}), ("linear", dict(scale=4.0)), ("base", dict(scale=8.0)),
+         ("wavelength", dict(scale=8.0, original_positions=8192, low=1.0, high=4.0)),
+         ("ramp", dict(scale=16.0, original_positions=4096, low=1.0, high=32.0)),
+         ("ramp", dict(scale=2.0, original_positions=64, low=1.0, high=32.0)),        # (the mix begins before the first pair)
+         ("wavelength", dict(scale=1.0, original_positions=100, low=0.5, high=50.0))]
+
+
+@pytest.mark.parametrize("d", [4, 16, 64, 128])
+@pytest.mark.parametrize("kind, args", KINDS)
+def test_frequencies(kind, args, d):
+    got = B.ooco_rope_frequencies(kind, d, base=500000.0, **args)
+    want, factor = S.rope_frequencies(kind, d, 500000.0, args.get("scale", 1.0), args.get("original_positions", 0.0), args.get("low", 1.0),
+                                      args.get("high", 2.0))
+    assert np.allclose(got["frequencies"], want, rtol=1e-12, atol=0) and math.isclose(got["factor"], factor, rel_tol=1e-14)
+
+
+def test_frequencies_that_are_stretched_lie_between_f_and_f_over_s():
+    plain = B.ooco_rope_frequencies("plain", 64)["frequencies"]
+    assert plain[0] == 1.0 and (np.diff(plain) < 0).all()
+    for kind, args in KINDS[1:]:
+        f = B.ooco_rope_frequencies(kind, 64, **args)["frequencies"]
+        assert (f <= plain * (1 + 1e-12)).all() and (f >= plain / args["scale"] * (1 - 1e-12)).all()
+
+
+@pytest.mark.parametrize("args, status", [
+    (("plain", 0), B.OOCO_ESHAPE), (("plain", 7), B.OOCO_ESHAPE), (("plain", 64, 1.0), B.OOCO_EINVAL), (("plain", 64, math.nan), B.OOCO_EINVAL),
+    (("linear", 64, 1e4, 0.5), B.OOCO_EINVAL), (("linear", 64, 1e4, math.inf), B.OOCO_EINVAL), (("base", 2, 1e4, 2.0), B.OOCO_ESHAPE),
+    (("wavelength", 64, 1e4, 2.0, 0.0, 1.0, 4.0), B.OOCO_EINVAL), (("ramp", 64, 1e4, 2.0, 4096, 4.0, 4.0), B.OOCO_EINVAL),
+    (("ramp", 64, 1e4, 2.0, 4096, 0.0, 4.0), B.OOCO_EINVAL)], ids=str)
+def test_frequencies_refused(args, status):
+    with pytest.raises(B.OocoError) as e:
+        B.ooco_rope_frequencies(*args)
+    assert e.value.status == status and e.value.message.startswith("ooco_rope_frequencies:")
+
+
+def test_kind_by_name():
+    with pytest.raises(ValueError):
+        B.ooco_rope_frequencies("other", 64)
+
+
+def test_calls_without_a_context_are_refused():
+    null = B._P()
+    for call in (lambda: B.ooco_tree_masks(null, None, None, None, None, None, 1, 1, 1, stream=0),
+                 lambda: B.ooco_rope_set(null, 64, 0, np.ones(32)),
+                 lambda: B.ooco_rope_append(null, None, None, None, None, None, None, None, None, None, None, 1, 1, stream=0),
+                 lambda: B.ooco_attn_tree(null, None, None, None, None, None, None, None, 1, None, 1, 1, stream=0),
+                 lambda: B.ooco_kv_compact(null, [], [], None, None, None, None, 4, 1, stream=0)):
+        with pytest.raises(B.OocoError) as e:
+            call()
+        assert e.value.status == B.OOCO_EINVAL
+
+
+# ------------------------------------------------------------------------------------------------ the oracle itself
+def test_masks_of_a_chain_are_causal_and_of_a_star_are_pairs():
+    chain, pos = S.tree_masks(np.arange(-1, 9), [0, 10], [5], 1)
+    assert [int(m) for m in chain[:, 0]] == [2 ** (t + 1) - 1 for t in range(10)] and pos.tolist() == list(range(5, 15))
+    star, pos = S.tree_masks(np.array([-1] + [0] * 9), [0, 10], [5], 1)
+    assert [int(m) for m in star[:, 0]] == [1] + [1 | 1 << t for t in range(1, 10)] and pos.tolist() == [5] + [6] * 9
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rotation_keeps_lengths_and_depends_on_distances(interleaved):
+    rng = np.random.default_rng(0)
+    f = S.rope_frequencies("plain", 32, 1e4)[0]
+    q, k = rng.standard_normal((2, 1, 1, 64))
+    dot = lambda a, b: float((S.rotate(q, [a], f, interleaved)[0] * S.rotate(k, [b], f, interleaved)[0]).sum())
+    assert math.isclose(float((S.rotate(q, [77], f, interleaved)[0] ** 2).sum()), float((q ** 2).sum()), rel_tol=1e-12)
+    assert math.isclose(dot(100, 90), dot(1010, 1000), rel_tol=1e-9) and not math.isclose(dot(100, 90), dot(100, 80), rel_tol=1e-3)
+
+
+def test_attention_of_a_chain_is_causal_attention():
+    from oracle import ref_numpy
+    from paper_2511_21862_amd import workloads as W
+
+    b = W.build_batch(Hq=4, Hkv=2, hd=64, q_lens=[5, 1, 7], ctx_lens=[20, 3, 0], num_blocks=9, seed=1)
+    want = ref_numpy.attn_mixed(b.q, b.k_cache, b.v_cache, b.block_tables, b.seq_lens, b.query_start_loc, b.ctx_lens)
+    kv = [[ref_numpy.widen_bf16(x) for x in W.gather_logical(b, i)] for i in range(3)]
+    parents = np.concatenate([np.arange(-1, n - 1) for n in (5, 1, 7)])
+    masks, _ = S.tree_masks(parents, b.query_start_loc, b.ctx_lens, 1)
+    got, size = S.attn_tree(ref_numpy.widen_bf16(b.q), [x[0] for x in kv], [x[1] for x in kv], b.query_start_loc, b.ctx_lens, masks)
+    assert np.allclose(got, want, rtol=1e-12, atol=1e-13) and (size >= np.abs(got) - 1e-12).all()
+
+
+@pytest.mark.parametrize("form", ["chain", "tree"])
+def test_verified_tokens_are_distributed_as_the_targets(form):
+    # the first token that a step yields, over many steps: its shares against the target's probabilities, within five deviations
+    rng = np.random.default_rng(3)
+    V, steps = 6, 40000
+    p, q = rng.dirichlet(np.ones(V)), rng.dirichlet(np.ones(V))
+    other = rng.dirichlet(np.ones(V))
+    seen = np.zeros(V)
+    for _ in range(steps):
+        if form == "chain":
+            tokens, parents, draft = np.array([0, rng.choice(V, p=q)]), None, np.stack([q, q])
+        else:
+            tokens, parents, draft = np.array([0, 2, 5, 1]), np.array([-1, 0, 0, 0]), None
+        n = len(tokens)
+        target = np.stack([p] + [other] * (n - 1))
+        _, _, out = S.verify_drafts(target, draft, tokens, parents, rng.random(n), rng.random(1), [0, n], n - 1)
+        seen[out[0, 0]] += 1
+    assert (np.abs(seen / steps - p) <= 5 * np.sqrt(p * (1 - p) / steps)).all(), (seen / steps, p)
