@@ -490,7 +490,7 @@ ooco_status ooco_rope_append(ooco_ctx *ctx, const void *q /*DEVICE*/, int64_t q_
  * out = softmax(scale * q K^T) V with fp32 statistics and accumulation, rounded to bf16; a row that sees nothing, or nothing but
  * scores of -inf, is zero.  A score of NaN or +inf reaches the rows and heads that see it, and no others.  V has to be finite in
  * every slot of a sequence below ctx_lens[i] + its nodes, also where a row does not see the token.
- * Any number of sequences and rows.  Partial results lie in the context's workspace (33 KiB per run of head_dim 128; fewer runs where
+ * Any number of sequences and rows.  Partial results lie in the context's workspace (260 KiB per compute unit with head_dim 128; less where
  * it is small, OOCO_ENOMEM where it holds none).  Same context, lengths and inputs: the same bits.  Two kernels. */
 ooco_status ooco_attn_tree(ooco_ctx *ctx, const void *q /*DEVICE*/, const void *k_cache /*DEVICE*/, const void *v_cache /*DEVICE*/,
                            const int32_t *block_tables /*DEVICE*/, const int32_t *query_start_loc /*DEVICE*/,

@@ -19,14 +19,15 @@ struct TreeArgs {
     const int32_t *ctx_lens;
     const uint64_t *masks;      // [total_q][words]
     uint16_t *out;
-    int32_t *merges;            // [runs][kMergeInts]: what the merge kernel has to do at the beginning of each run
+    int32_t *merges;            // [runs][4]: parts of the unit that the merge kernel has for the run, its first row, rows, kv head
     float *part_acc;            // [2 * runs][columns of a tile][hd]  un-normalised partial outputs
-    float *part_ml;             // [2 * runs][columns of a tile][2]   (running maximum in log2 units, sum)
+    float *part_ml;             // [2 * runs][columns of a tile][2]   (reference in log2 units, sum)
     int64_t num_blocks;
     int32_t Hq, Hkv, g, hd;
     int32_t max_blocks_per_seq;
     int32_t num_seqs, total_q, words;
     int32_t runs_log2;          // runs of the line: 1 << runs_log2 workgroups
+    int32_t tile_rows;          // rows of the widest tile
     float scale_log2e;          // softmax scale * log2(e)
 };
 // Runs (a power of two) that a workspace of ws_bytes allows on num_cus compute units, as their logarithm; < 0: none.

@@ -5,27 +5,31 @@
 // O^T[dim][query column] = V^T P^T; a query column is a (row, head of the GQA group) pair, so that the K and V of a token are
 // fetched once for all nodes and heads that see it.  One pass over the keys with the running maximum and sum of the softmax.
 //
-// Work: the columns of a sequence are cut into tiles, as few as hold them: of 32, 64 or 128 columns, a wave of the workgroup having
-// 32; the waves that columns leave over share the tokens of a step.  Unit = (tile, kv head), walked in steps of 128 tokens.  The
-// units of all sequences, steps end to end, form a line that is cut into equal runs, a workgroup each; where a run ends inside a
-// unit, partial results meet in the merge kernel.  The lengths are read and the line is laid out on the device by every workgroup for
-// itself: no plan and no host copy of lengths that the last step's verification has just decided.
-//   32 columns      the four waves have 32 tokens of a step each, and load K and V from the cache to the registers of the matrix
-//                   instructions: nothing is shared, so nobody waits for anybody
+// Work: the columns of a sequence are cut into tiles of 128, the last as wide as 32, 64 or 128 columns have to be; each of a workgroup's
+// four waves has 32 columns, and the waves that columns leave over share the tokens.  Unit = (kv head, tile), walked in steps of 128
+// tokens.  The units of all sequences, steps end to end, form a line that is cut into equal runs, a workgroup each, two to a compute unit;
+// where a run ends inside a unit, partial results meet in the merge kernel.  The lengths are read and the line is laid out on the device by
+// every workgroup for itself: no plan and no host copy of lengths that the last step's verification has just decided.
+//   32 columns      every wave loads K and V of its own tokens from the cache to the registers of the matrix instructions: nothing is
+//                   shared, so nobody waits for anybody, and a compute unit has 128 KiB on their way
 //   64, 128         K and V of 64 tokens at a time go through LDS, for two or four waves, by direct loads into the other of two buffers
+//   128             the products of 32 tokens run beside the exponentials of 32 others (see region)
 #include "ooco_device.h"
 #include "ooco_internal.h"
 #include "ooco_spec.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace ooco {
 
-constexpr int kTreeCols = 128;        // query columns of the widest tile
-constexpr int kTreeThreads = 256;
-constexpr int kTreeStep = 128;        // tokens of a step
-constexpr int kMergeInts = 8;
-constexpr int kMinRun = 1;            // steps of a run, at least
+constexpr int kTreeWaves = 4;
+constexpr int kTreeThreads = 64 * kTreeWaves;
+constexpr int kTreeCols = 32 * kTreeWaves;   // query columns of the widest tile
+constexpr int kTreeStep = 128;               // tokens of a step
+constexpr int kMinRun = 1;                   // steps of a run, at least
+constexpr int kMergeInts = 4;
+constexpr int kMergeThreads = 256;
 
 // The largest of a lane's sixteen scores, NaN if one is.  (v_maximum3_f32, which needs no operand quieted.  Not the asm of max16:
 // the waits between a matrix instruction and what reads its result are the compiler's, which does not see into asm.)
@@ -39,10 +43,11 @@ OOCO_DEV float largest(const f32x16 &s)
 
 // What a sequence has on the line.
 struct TreeSeq {
-    int q0, n, ctx, len, steps;          // len: tokens that exist, the nodes among them
-    int waves;                           // of 32 columns that a tile has: 1, 2 or 4
-    int tile_rows, tiles;
-    int64_t units;                       // steps of all its units
+    int q0, n, ctx, len, steps;      // len: tokens that exist, the nodes among them
+    int tile_rows, tiles;            // rows of a tile but the last
+    int last_waves;                  // waves that have columns of the last tile: 1, 2 or 4
+    int64_t units;                   // steps of all its units
+    OOCO_DEV int unit_waves(int tile) const { return tile == tiles - 1 ? last_waves : kTreeWaves; }
 };
 OOCO_DEV TreeSeq tree_seq(const TreeArgs &p, int q0, int q1, int ctx)
 {
@@ -52,15 +57,18 @@ OOCO_DEV TreeSeq tree_seq(const TreeArgs &p, int q0, int q1, int ctx)
     if (q0 < 0 || s.n < 0 || s.n > p.total_q - q0) s.n = 0;
     const int cap = (int)min((int64_t)p.max_blocks_per_seq * kBlockSize, (int64_t)INT32_MAX - 1024);
     s.ctx = min(max(ctx, 0), cap);
-    s.len = min(s.ctx + min(s.n, 64 * p.words), cap);
-    // (rows of a group of heads that does not divide 32: a tile of 32 columns has fewer than 32 of them)
-    s.waves = s.n <= 32 / p.g ? 1 : s.n <= 64 / p.g ? 2 : 4;
-    s.tile_rows = 32 * s.waves / p.g;
-    s.tiles = (s.n + s.tile_rows - 1) / s.tile_rows;
+    s.len = (int)min((int64_t)s.ctx + min(s.n, 64 * p.words), (int64_t)cap);
     s.steps = (s.len + kTreeStep - 1) / kTreeStep;
+    s.tile_rows = p.tile_rows;       // (a group of heads that does not divide 128: the columns behind the last whole row are none)
+    s.tiles = (s.n + s.tile_rows - 1) / s.tile_rows;
+    const int last_cols = (s.n - (s.tiles - 1) * s.tile_rows) * p.g;
+    s.last_waves = last_cols <= 32 ? 1 : last_cols <= 64 ? 2 : 4;
     s.units = (int64_t)s.tiles * p.Hkv * s.steps;
     return s;
 }
+// floor(a / b) of numbers below 2^53: a correctly rounded quotient does not reach the next integer.  (The compiler's 64-bit division
+// is some hundred instructions, and instructions are what a small launch waits for.)
+OOCO_DEV int64_t quotient(int64_t a, int64_t b) { return (int64_t)((double)a / (double)b); }
 
 // The line: its length, and the sequence that holds position `at(total)` of it, with the position of that sequence's first step.
 // All threads of the workgroup call it together.
@@ -143,7 +151,7 @@ struct TreeRuns {
     bool split;      // the line is cut into all runs there are, else into runs of kMinRun steps
     OOCO_DEV TreeRuns(int64_t total_, int log2_) : total(total_), log2(log2_), split(total_ >= ((int64_t)kMinRun << log2_)) {}
     OOCO_DEV int64_t first(int w) const { return split ? (total * w) >> log2 : min(total, (int64_t)w * kMinRun); }
-    OOCO_DEV int holding(int64_t x) const { return split ? (int)((((x + 1) << log2) - 1) / total) : (int)(x / kMinRun); }
+    OOCO_DEV int holding(int64_t x) const { return split ? (int)quotient(((x + 1) << log2) - 1, total) : (int)(x / kMinRun); }
 };
 
 // What a wave does with 32 tokens, whichever way they come: its 32 query columns' share of the softmax and of the output.
@@ -154,6 +162,7 @@ struct TreeWave {
     u32x4 qb[KS];
     f32x16 O[MB];
     float m, lsum;                       // reference of the column's weights in log2 units, this lane's share of their sum
+    float scale;                         // of scores, to log2 units
     const uint64_t *mask;
 
     OOCO_DEV void begin(const TreeArgs &p, int64_t q_row, int head, int h)
@@ -162,6 +171,11 @@ struct TreeWave {
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) qb[ks] = qp[2 * ks + h];
         mask = p.masks + q_row * p.words;
+        scale = p.scale_log2e;
+        none();
+    }
+    OOCO_DEV void none()   // no tokens
+    {
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
@@ -169,61 +183,71 @@ struct TreeWave {
         m = -1e30f;   // (finite: tokens that a column does not see weigh nothing, where -inf - -inf would make them NaN)
         lsum = 0.f;
     }
-    // Bit i: the column sees token tok0 + i.  tok0 + 32 > ctx.
-    OOCO_DEV uint32_t sees(int words, int tok0, int ctx, int len) const
+    // Hides the scores of tokens that the column does not see.  Register r of S is token tok0 + 16 (r / 8) + 8 h + r % 8.
+    OOCO_DEV void hide(f32x16 &S, int words, int tok0, int ctx, int len, int h) const
     {
         const int j0 = tok0 - ctx;   // node that token tok0 is (negative: cached)
-        uint32_t bits;
+        if (j0 <= -32) return;
+        uint32_t bits;               // bit i: the column sees token tok0 + i
         if (j0 >= 0) {
             const int k = j0 >> 6, sh = j0 & 63;
             uint64_t b = k < words ? mask[k] >> sh : 0;
             if (sh > 32 && k + 1 < words) b |= mask[k + 1] << (64 - sh);
             bits = (uint32_t)b;
         } else {
-            bits = ((uint32_t)mask[0] << -j0) | ((1u << -j0) - 1u);   // (-31 <= j0)
+            bits = ((uint32_t)mask[0] << -j0) | ((1u << -j0) - 1u);
         }
         const int left = len - tok0;   // tokens that exist
         if (left < 32) bits &= left > 0 ? (1u << left) - 1u : 0u;
-        return bits;
-    }
-    // Register r of S is token 16 (r / 8) + 8 h + r % 8 of the 32.
-    OOCO_DEV static void hide(f32x16 &S, uint32_t bits, int h)
-    {
         bits >>= 8 * h;
 #pragma unroll
         for (int r = 0; r < 16; ++r) S[r] = (bits >> (16 * (r / 8) + r % 8)) & 1u ? S[r] : -INFINITY;
     }
-    // Scores to weights.  The reference moves only where a score exceeds it by 2^8: weights up to 2^8 are as exact in bf16 and fp32
-    // as below 1, and the division at the end takes the reference out.
-    OOCO_DEV void weights(const f32x16 &S, float scale, u32x4 (&P)[2])
+    // Weights are taken against a reference that moves only where scores exceed it by 2^8: weights up to 2^8 are as exact in bf16
+    // and fp32 as below 1, and the division at the end takes the reference out.
+    OOCO_DEV static constexpr float slack() { return 8.0f; }
+    OOCO_DEV float top(const f32x16 &S) const
     {
         float x, y;
         swap32(largest(S), x, y);
-        const float top = __builtin_elementwise_maximum(x, y) * scale;
-        if (__any(top > m + 8.0f)) {
-            const float m_new = fmaxf(m, top), alpha = fast_exp2(m - m_new);
-            m = m_new;
-            lsum *= alpha;
+        return __builtin_elementwise_maximum(x, y) * scale;
+    }
+    OOCO_DEV void move(float to)
+    {
+        const float m_new = fmaxf(m, to), alpha = fast_exp2(m - m_new);
+        m = m_new;
+        lsum *= alpha;
 #pragma unroll
-            for (int mb = 0; mb < MB; ++mb)
+        for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) O[mb][r] *= alpha;
-        }
+            for (int r = 0; r < 16; ++r) O[mb][r] *= alpha;
+    }
+    // Scores to weights, and this lane's sum of them.
+    OOCO_DEV float weights(const f32x16 &S, u32x4 (&P)[2]) const
+    {
+        float sum = 0.f;
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             float e[8];
 #pragma unroll
             for (int r = 0; r < 8; ++r) {
                 e[r] = fast_exp2(__builtin_fmaf(S[8 * b + r], scale, -m));
-                lsum += e[r];
+                sum += e[r];
             }
             P[b] = u32x4{pack2_bf16(e[0], e[1]), pack2_bf16(e[2], e[3]), pack2_bf16(e[4], e[5]), pack2_bf16(e[6], e[7])};
         }
+        return sum;
+    }
+    OOCO_DEV void add(const f32x16 &S, u32x4 (&P)[2])
+    {
+        const float t = top(S);
+        if (__any(t > m + slack())) move(t);
+        lsum += weights(S, P);
     }
 };
 
-// A tile of K or of V (one block, one kv head) from the cache into LDS, HD / 32 loads of 16 bytes per lane: 1 KiB each, contiguous in LDS from
-// dst on.  off[n]: the lane's place in the tile for load n, less n KiB (the instruction's offset counts for both addresses).
+// A tile of K or of V (one block, one kv head) from the cache into LDS, HD / 32 loads of 16 bytes per lane: 1 KiB each, contiguous in LDS
+// from dst on.  off[n]: the lane's place in the tile for load n, less n KiB (the instruction's offset counts for both addresses).
 template <int HD>
 OOCO_DEV void tile_to_lds(const char *base, uint32_t dst, const uint32_t (&off)[4])
 {
@@ -243,7 +267,9 @@ OOCO_DEV void tile_to_lds(const char *base, uint32_t dst, const uint32_t (&off)[
                      : "memory");
 }
 
-constexpr int kStageBlocks = 4;   // KV blocks that go through LDS at a time
+constexpr int kStageTokens = 64;                              // tokens that go through LDS at a time
+constexpr int kStageBlocks = kStageTokens / kBlockSize;       // a block for each wave to bring
+static_assert(kStageBlocks == kTreeWaves && kTreeStep % kStageTokens == 0, "stages of a step");
 
 template <int HD>
 __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(const TreeArgs p)
@@ -252,18 +278,21 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(const TreeArgs p)
     constexpr int KS = Wave::KS, MB = Wave::MB;
     constexpr int ROW = HD + 4;                   // floats of a column in LDS (padded: the lanes of a wave are columns)
     constexpr int CH = 2 * HD;                    // 16-byte pieces of a tile of K or V
+    constexpr int STAGE = kStageBlocks * CH;
     constexpr int64_t kTile = (int64_t)HD * kBlockSize;
-    constexpr int kSlab = 4 * 32 * ROW * 4, kStage = 2 * 2 * kStageBlocks * CH * 16;
+    constexpr int kSlab = kTreeWaves * 32 * ROW * 4, kStage = 2 * 2 * STAGE * 16;
     __shared__ __align__(16) unsigned char lds[kSlab > kStage ? kSlab : kStage];
-    __shared__ float stat[4][32][2];
+    __shared__ float stat[kTreeWaves][32][2];
     float (*const slab)[32][ROW] = reinterpret_cast<float (*)[32][ROW]>(lds);           // [wave][column][dim]
-    u32x4 *const ldsK = reinterpret_cast<u32x4 *>(lds), *const ldsV = ldsK + 2 * kStageBlocks * CH;   // [buffer][block][piece]
+    u32x4 *const ldsK = reinterpret_cast<u32x4 *>(lds), *const ldsV = ldsK + 2 * STAGE;   // [buffer][block][piece]
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, h = lane >> 5;
     const int g = p.g;
-    const int w = blockIdx.x;
+    // Runs next to each other on the line are on one XCD (workgroup b runs on XCD b % 8): the tiles of one sequence and kv head walk the
+    // same tokens at about the same time, and share an L2.
+    const int w = p.runs_log2 >= 3 ? (int)((blockIdx.x & 7) << (p.runs_log2 - 3)) + (int)(blockIdx.x >> 3) : (int)blockIdx.x;
 
     int seq = 0;
     int64_t start = 0;
@@ -273,7 +302,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(const TreeArgs p)
     const int64_t lo = runs.first(w), hi = runs.first(w + 1);
     int32_t *const merge = p.merges + (int64_t)w * kMergeInts;
     if (lo >= hi) {
-        if (tid == 0) merge[1] = 0;
+        if (tid == 0) merge[0] = 0;
         return;
     }
     // K operand row col -> block (col >> 4) of the 32 tokens, slot with bits 2 and 3 swapped, so that register r of S^T is token
@@ -292,6 +321,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(const TreeArgs p)
     const uint32_t ldsV_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)ldsV;
 
     int64_t pos = lo;
+    int parts = 0;   // of the unit that the run begins inside of, if the run is the second that works on it
     seq = __builtin_amdgcn_readfirstlane(seq);
     TreeSeq s = tree_seq_at(p, seq);
     while (pos < hi) {
@@ -300,50 +330,70 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(const TreeArgs p)
             ++seq;
             s = tree_seq_at(p, seq);
         }
-        const int unit = (int)((pos - start) / s.steps);
+        const int unit = (int)quotient(pos - start, s.steps);
         const int s0 = (int)(pos - start - (int64_t)unit * s.steps);
         const int s1 = (int)min((int64_t)s.steps, s0 + (hi - pos));
-        const int tile = unit / p.Hkv, kvh = unit - tile * p.Hkv;
+        const int kvh = s.tiles == 1 ? unit : unit / s.tiles, tile = unit - kvh * s.tiles;
+        const int waves = s.unit_waves(tile);
         const int row0 = tile * s.tile_rows, rows = min(s.tile_rows, s.n - row0);
 
-        const int cw = wave & (s.waves - 1), kw = wave / s.waves;   // this wave's columns, and its tokens of a step
-        const int c = 32 * cw + col;
+        const int cw = wave & (waves - 1), kw = wave / waves;   // this wave's columns, and its share of the tokens
         // (32 columns of a tile are 32 columns of its rows end to end; columns behind the last row repeat it)
-        const int c_row = min(c / g, rows - 1), c_head = c % g;
+        const int c = 32 * cw + col, c_row = min(c / g, rows - 1), c_head = c % g;
+        const int64_t q_row = (int64_t)s.q0 + row0 + c_row;
 
         const int nblk = (s.len + kBlockSize - 1) / kBlockSize;
         const const_i32_ptr table = scalar_ptr(p.block_tables + (int64_t)seq * p.max_blocks_per_seq);
-        auto id_at = [&](int block) -> int64_t {   // of the block of the sequence; blocks past the end: the last one
-            const int64_t id = table[min(block, nblk - 1)];
-            return min(max(id, (int64_t)0), p.num_blocks - 1);
-        };
+        const int last_id = (int)min(p.num_blocks, (int64_t)INT32_MAX) - 1;
+        auto id_at = [&](int block) -> int { return table[min(block, nblk - 1)]; };   // blocks past the end: the last one
+        auto bytes_at = [&](int id) -> int64_t { return ((int64_t)min(max(id, 0), last_id) * p.Hkv + kvh) * (kTile * 2); };
+        const char *const k_cache = reinterpret_cast<const char *>(p.k_cache), *const v_cache = reinterpret_cast<const char *>(p.v_cache);
         Wave x;
         __syncthreads();   // (LDS: the last unit's results have been read)
-        if (s.waves == 1) {
-            x.begin(p, (int64_t)s.q0 + row0 + c_row, kvh * g + c_head, h);
-            for (int st = s0; st < s1; ++st) {
-                const int tok0 = st * kTreeStep + 32 * wave;
-                if (tok0 >= s.len) break;
-                const int64_t t0 = (id_at(tok0 / kBlockSize) * p.Hkv + kvh) * kTile, t1 = (id_at(tok0 / kBlockSize + 1) * p.Hkv + kvh) * kTile;
+        if (waves == 1) {
+            // 32 tokens, two blocks, at a time: those of the run from 32 * wave on, every 128.  Loads behind the wave's last tokens fetch
+            // those again, so that every turn has the same number of loads on their way.
+            const int t_end = min(4 * s1, (s.len + 31) / 32);
+            int t = 4 * s0 + wave;
+            x.begin(p, q_row, kvh * g + c_head, h);
+            if (t < t_end) {
+                const int t_last = t + (t_end - 1 - t) / kTreeWaves * kTreeWaves;
+                int ida = id_at(2 * t), idb = id_at(2 * t + 1);
                 u32x4 kr[KS], vr[2][MB];
-                const u32x4 *const kp = reinterpret_cast<const u32x4 *>(p.k_cache + (ku ? t1 : t0));
+                int64_t at0, at1;
+                auto load_k = [&]() {
+                    at0 = bytes_at(ida);
+                    at1 = bytes_at(idb);
+                    const u32x4 *const kp = reinterpret_cast<const u32x4 *>(k_cache + (ku ? at1 : at0));
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) kr[ks] = kp[(2 * ks + h) * kBlockSize + kslot];
+                    for (int ks = 0; ks < KS; ++ks) kr[ks] = __builtin_nontemporal_load(&kp[(2 * ks + h) * kBlockSize + kslot]);
+                };
+                auto load_v = [&]() {
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const u32x4 *const vp = reinterpret_cast<const u32x4 *>(p.v_cache + (b ? t1 : t0));
+                    for (int b = 0; b < 2; ++b) {
+                        const u32x4 *const vp = reinterpret_cast<const u32x4 *>(v_cache + (b ? at1 : at0));
 #pragma unroll
-                    for (int mb = 0; mb < MB; ++mb) vr[b][mb] = vp[2 * (32 * mb + col) + h];
-                }
-                f32x16 S;
+                        for (int mb = 0; mb < MB; ++mb) vr[b][mb] = __builtin_nontemporal_load(&vp[2 * (32 * mb + col) + h]);
+                    }
+                };
+                auto next_ids = [&](int next) {
+                    ida = id_at(2 * min(next, t_last));
+                    idb = id_at(2 * min(next, t_last) + 1);
+                };
+                load_k();
+                __builtin_amdgcn_sched_barrier(kNoVmem);   // (the scores wait for K alone)
+                load_v();
+                next_ids(t + kTreeWaves);
+                for (; t < t_end; t += kTreeWaves) {
+                    const int tok0 = 32 * t, left = s.len - tok0;
+                    f32x16 S;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) S[r] = 0.f;
+                    for (int r = 0; r < 16; ++r) S[r] = 0.f;
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks)
-                    S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kr[ks]), __builtin_bit_cast(bf16x8, x.qb[ks]), S, 0, 0, 0);
-                if (tok0 + 32 > s.ctx) {   // nodes among the tokens
-                    Wave::hide(S, x.sees(p.words, tok0, s.ctx, s.len), h);
-                    const int left = s.len - tok0;
+                    for (int ks = 0; ks < KS; ++ks)
+                        S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kr[ks]), __builtin_bit_cast(bf16x8, x.qb[ks]), S, 0, 0, 0);
+                    load_k();
+                    x.hide(S, p.words, tok0, s.ctx, s.len, h);
                     if (left < 32) {
 #pragma unroll
                         for (int b = 0; b < 2; ++b) {   // (slots past the end may hold anything, and 0 * NaN is NaN)
@@ -356,39 +406,34 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(const TreeArgs p)
                             for (int mb = 0; mb < MB; ++mb) vr[b][mb] &= keep;
                         }
                     }
+                    u32x4 P[2];
+                    x.add(S, P);
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+#pragma unroll
+                        for (int mb = 0; mb < MB; ++mb)
+                            x.O[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vr[b][mb]), __builtin_bit_cast(bf16x8, P[b]),
+                                                                              x.O[mb], 0, 0, 0);
+                    load_v();
+                    next_ids(t + 2 * kTreeWaves);
                 }
-                u32x4 P[2];
-                x.weights(S, p.scale_log2e, P);
-#pragma unroll
-                for (int b = 0; b < 2; ++b)
-#pragma unroll
-                    for (int mb = 0; mb < MB; ++mb)
-                        x.O[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vr[b][mb]), __builtin_bit_cast(bf16x8, P[b]),
-                                                                          x.O[mb], 0, 0, 0);
             }
         } else {
-            // 64 tokens at a time: wave i brings block i of the four
-            const int f0 = 2 * s0, f1 = min(2 * s1, (s.len + 63) / 64);   // stages (the last step may have one)
-            auto stage = [&](int f) {
-                const uint64_t tile_bytes = (uint64_t)(id_at(kStageBlocks * f + wave) * p.Hkv + kvh) * (kTile * 2);
-                const uint32_t at = (uint32_t)(((f & 1) * kStageBlocks + wave) * CH * 16);
-                const char *const kb = reinterpret_cast<const char *>(p.k_cache) + tile_bytes;
-                const char *const vb = reinterpret_cast<const char *>(p.v_cache) + tile_bytes - kBias;
-                tile_to_lds<HD>(kb, ldsK_at + at, k_off);
-                tile_to_lds<HD>(vb, ldsV_at + at, v_off);
+            // Stages of 64 tokens, f0 .. f1 - 1 (the sequence's last step may have one); wave i brings block i of a stage.
+            const int f0 = 2 * s0, f1 = min(2 * s1, (s.len + kStageTokens - 1) / kStageTokens);
+            auto stage_id = [&](int f) -> int { return id_at(kStageBlocks * f + wave); };
+            auto stage_k = [&](int f, int id) { tile_to_lds<HD>(k_cache + bytes_at(id), ldsK_at + (uint32_t)((f & 1) * STAGE + wave * CH) * 16u, k_off); };
+            auto stage_v = [&](int f, int id) {
+                tile_to_lds<HD>(v_cache + bytes_at(id) - kBias, ldsV_at + (uint32_t)((f & 1) * STAGE + wave * CH) * 16u, v_off);
             };
-            stage(f0);
-            x.begin(p, (int64_t)s.q0 + row0 + c_row, kvh * g + c_head, h);
-            const bool used = 32 * cw < rows * g;   // (the last tile may leave waves without columns: they only bring blocks)
-            for (int f = f0; f < f1; ++f) {
+            // Everybody's loads have landed, and everybody is done with what came before; V of stage f is used next.
+            auto arrive = [&](int f) {
                 asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-                __syncthreads();   // everybody's tiles have landed, and everybody is done with the other buffer
-                if (f + 1 < f1) stage(f + 1);
-                const u32x4 *const K = ldsK + (f & 1) * kStageBlocks * CH;
-                u32x4 *const V = ldsV + (f & 1) * kStageBlocks * CH;
-                if (64 * f + 64 > s.len) {   // (slots past the end may hold anything, and 0 * NaN is NaN)
-                    for (int i = tid; i < kStageBlocks * CH; i += kTreeThreads) {
-                        const int first = 64 * f + 16 * (i / CH) + 8 * (i % CH / HD);
+                __syncthreads();
+                if (kStageTokens * (f + 1) > s.len) {   // (slots past the end may hold anything, and 0 * NaN is NaN)
+                    u32x4 *const V = ldsV + (f & 1) * STAGE;
+                    for (int i = tid; i < STAGE; i += kTreeThreads) {
+                        const int first = kStageTokens * f + 16 * (i / CH) + 8 * (i % CH / HD);
                         u32x4 keep;
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
@@ -397,25 +442,132 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(const TreeArgs p)
                     }
                     __syncthreads();
                 }
-                if (!used) continue;
-                for (int half = s.waves == 4 ? 0 : kw; half < (s.waves == 4 ? 2 : kw + 1); ++half) {
-                    const int tok0 = 64 * f + 32 * half;
+            };
+            // operand i of the product of 32 tokens (half a stage) with K and of their weights with V
+            auto k_operand = [&](int f, int half, int i) -> u32x4 { return ldsK[(f & 1) * STAGE + (2 * half + ku) * CH + (2 * i + h) * kBlockSize + kslot]; };
+            auto v_operand = [&](int f, int half, int i) -> u32x4 { return ldsV[(f & 1) * STAGE + (2 * half + i / MB) * CH + h * HD + 32 * (i % MB) + col]; };
+            const bool used = 32 * cw < rows * g;   // (columns behind the last row: such waves only bring blocks)
+            int id0 = stage_id(f0), id1 = stage_id(f0 + 1);
+            stage_k(f0, id0);
+            stage_v(f0, id0);
+            if (waves == 2) {
+                x.begin(p, q_row, kvh * g + c_head, h);
+                for (int f = f0; f < f1; ++f) {   // a half stage for each of the two waves that have the same columns
+                    arrive(f);
+                    if (f + 1 < f1) {
+                        stage_k(f + 1, id1);
+                        stage_v(f + 1, id1);
+                        id1 = stage_id(f + 2);
+                    }
+                    if (!used) continue;
                     f32x16 S;
 #pragma unroll
                     for (int r = 0; r < 16; ++r) S[r] = 0.f;
 #pragma unroll
                     for (int ks = 0; ks < KS; ++ks)
-                        S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, K[(2 * half + ku) * CH + (2 * ks + h) * kBlockSize + kslot]),
-                                                                    __builtin_bit_cast(bf16x8, x.qb[ks]), S, 0, 0, 0);
-                    if (tok0 + 32 > s.ctx) Wave::hide(S, x.sees(p.words, tok0, s.ctx, s.len), h);
+                        S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k_operand(f, kw, ks)), __builtin_bit_cast(bf16x8, x.qb[ks]), S, 0, 0, 0);
+                    x.hide(S, p.words, kStageTokens * f + 32 * kw, s.ctx, s.len, h);
                     u32x4 P[2];
-                    x.weights(S, p.scale_log2e, P);
+                    x.add(S, P);
 #pragma unroll
-                    for (int b = 0; b < 2; ++b)
+                    for (int i = 0; i < KS; ++i)
+                        x.O[i % MB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v_operand(f, kw, i)), __builtin_bit_cast(bf16x8, P[i / MB]),
+                                                                              x.O[i % MB], 0, 0, 0);
+                }
+            } else {
+                // Both halves of every stage, in a pipeline: a region multiplies the weights of one half by V and computes the scores
+                // of the half after next while the vector ALU turns the scores of the half between them into weights.  K runs a stage ahead of V.
+                if (f0 + 1 < f1) stage_k(f0 + 1, id1);
+                x.begin(p, q_row, kvh * g + c_head, h);
+                int id2 = stage_id(f0 + 2);
+                constexpr int AHEAD = 2;   // products ahead of which an operand is asked for
+                u32x4 ring[AHEAD];
+                auto operand = [&](auto pv, auto qk, int i, int fv, int hv, int fk, int hk) -> u32x4 {
+                    constexpr bool PV = decltype(pv)::value, QK = decltype(qk)::value;
+                    const int j = PV && QK ? i / 2 : i;
+                    return QK && (!PV || (i & 1) == 0) ? k_operand(fk, hk, j) : v_operand(fv, hv, j);
+                };
+                // PV: weights Pu by V, half hv of stage fv; NEXT: scores Ss to weights Pn; QK: scores Sq of half hk of stage fk.  Returns this lane's
+                // sum of Pn.
+                auto region = [&](auto pv, auto next, auto qk, const u32x4 (&Pu)[2], int fv, int hv, const f32x16 &Ss, u32x4 (&Pn)[2], f32x16 &Sq,
+                                  int fk, int hk) -> float {
+                    constexpr bool PV = decltype(pv)::value, NEXT = decltype(next)::value, QK = decltype(qk)::value;
+                    constexpr int NM = (PV ? KS : 0) + (QK ? KS : 0);
+                    float e[16], sum = 0.f;
+                    auto vector_work = [&](int r) {   // of score r, one stage later per two scores
+                        if (r < 16) e[r] = __builtin_fmaf(Ss[r], x.scale, -x.m);
+                        const int a = r - 2;
+                        if (a >= 0 && a < 16) e[a] = fast_exp2(e[a]);
+                        const int y = r - 4;
+                        if (y >= 0 && y < 16 && (y & 1)) {
+                            Pn[y / 8][(y % 8) / 2] = pack2_bf16(e[y - 1], e[y]);
+                            sum += e[y - 1] + e[y];
+                        }
+                    };
+                    constexpr int CALLS = 20, OVER = NM - 2;   // calls of vector_work for 16 scores, products that they are spread over
 #pragma unroll
-                        for (int mb = 0; mb < MB; ++mb)
-                            x.O[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, V[(2 * half + b) * CH + h * HD + 32 * mb + col]),
-                                                                              __builtin_bit_cast(bf16x8, P[b]), x.O[mb], 0, 0, 0);
+                    for (int i = 0; i < AHEAD; ++i) ring[i] = operand(pv, qk, i, fv, hv, fk, hk);
+#pragma unroll
+                    for (int i = 0; i < NM; ++i) {
+                        const int j = PV && QK ? i / 2 : i;
+                        const bf16x8 op = __builtin_bit_cast(bf16x8, ring[i % AHEAD]);
+                        if (QK && (!PV || (i & 1) == 0)) {
+                            f32x16 z;
+#pragma unroll
+                            for (int r = 0; r < 16; ++r) z[r] = 0.f;
+                            Sq = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, __builtin_bit_cast(bf16x8, x.qb[j]), j == 0 ? z : Sq, 0, 0, 0);
+                        } else {
+                            x.O[j % MB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, __builtin_bit_cast(bf16x8, Pu[j / MB]), x.O[j % MB], 0, 0, 0);
+                        }
+                        if (i + AHEAD < NM) ring[i % AHEAD] = operand(pv, qk, i + AHEAD, fv, hv, fk, hk);
+                        if constexpr (NEXT) {
+#pragma unroll
+                            for (int r = i * CALLS / OVER; r < (i + 1) * CALLS / OVER; ++r)
+                                if (r < CALLS) vector_work(r);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                    return sum;
+                };
+                const auto yes = std::true_type();
+                const auto no = std::false_type();
+                // The weights of a half were computed against a reference that was too low for some column (their sum is more than 2^8, infinite
+                // or NaN): once more, against the half's maximum.
+                auto settle = [&](const f32x16 &S, u32x4 (&P)[2], float sum) {
+                    if (!__all(sum <= 256.0f)) {
+                        x.move(x.top(S));
+                        sum = x.weights(S, P);
+                    }
+                    x.lsum += sum;
+                };
+                auto hide = [&](f32x16 &S, int f, int half) { x.hide(S, p.words, kStageTokens * f + 32 * half, s.ctx, s.len, h); };
+                f32x16 S0 = {}, S1 = {};
+                u32x4 P0[2] = {}, P1[2] = {};
+                arrive(f0);
+                if (used) {
+                    region(no, no, yes, P0, 0, 0, S0, P0, S0, f0, 0);
+                    hide(S0, f0, 0);
+                    x.m = fmaxf(x.m, x.top(S0));
+                    settle(S0, P0, region(no, yes, yes, P0, 0, 0, S0, P0, S1, f0, 1));
+                }
+                for (int f = f0; f < f1 - 1; ++f) {
+                    if (f > f0) arrive(f);
+                    else __syncthreads();   // (K of stage f0 has been used)
+                    if (f + 2 < f1) stage_k(f + 2, id2);
+                    stage_v(f + 1, id1);
+                    id1 = id2;
+                    id2 = stage_id(f + 3);
+                    if (!used) continue;
+                    hide(S1, f, 1);
+                    settle(S1, P1, region(yes, yes, yes, P0, f, 0, S1, P1, S0, f + 1, 0));
+                    hide(S0, f + 1, 0);
+                    settle(S0, P0, region(yes, yes, yes, P1, f, 1, S0, P0, S1, f + 1, 1));
+                }
+                if (f1 - 1 > f0) arrive(f1 - 1);
+                if (used) {
+                    hide(S1, f1 - 1, 1);
+                    settle(S1, P1, region(yes, yes, no, P0, f1 - 1, 0, S1, P1, S0, 0, 0));
+                    region(yes, no, no, P1, f1 - 1, 1, S0, P0, S0, 0, 0);
                 }
             }
             __syncthreads();   // (the buffers become the slab)
@@ -437,18 +589,18 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(const TreeArgs p)
         __syncthreads();
         constexpr int PER = HD / 8;               // dims of a thread: eight threads have a column
         const bool whole = s0 == 0 && s1 == s.steps;
-        const int64_t slot = 2 * (int64_t)w + (pos == lo ? 0 : 1);
-        for (int i = 0; i < s.waves; ++i) {
+        const int64_t slot = 2 * (int64_t)w + (s0 == 0 ? 1 : 0);   // (a run has one unit that begins before it, and one that ends behind it)
+        for (int i = 0; i < waves; ++i) {
             const int oc = 32 * i + tid / 8, od = (tid & 7) * PER;
             const int o_row = oc / g, o_head = oc - o_row * g;
             if (o_row >= rows) break;
             float M = -INFINITY;
-            for (int k = i; k < 4; k += s.waves) M = fmaxf(M, stat[k][oc & 31][0]);
+            for (int k = i; k < kTreeWaves; k += waves) M = fmaxf(M, stat[k][oc & 31][0]);
             float l = 0.f;
             f32x4 acc[PER / 4];
 #pragma unroll
             for (int j = 0; j < PER / 4; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-            for (int k = i; k < 4; k += s.waves) {
+            for (int k = i; k < kTreeWaves; k += waves) {
                 const float weight = fast_exp2(stat[k][oc & 31][0] - M);
                 l += stat[k][oc & 31][1] * weight;
 #pragma unroll
@@ -474,52 +626,59 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(const TreeArgs p)
                 }
             }
         }
-        if (pos == lo && tid == 0) {
-            // the run that the second part of a unit is in says where all its parts are
-            const int64_t unit_lo = pos - s0;
-            int parts = 0;
-            if (s0 > 0 && w > 0 && unit_lo >= runs.first(w - 1)) {
-                parts = runs.holding(unit_lo + s.steps - 1) - (w - 1) + 1;
-                merge[0] = unit_lo == runs.first(w - 1) ? 0 : 1;   // which part of run w - 1 it is
-                merge[2] = s.q0 + row0;
-                merge[3] = rows;
-                merge[4] = kvh;
+        if (s0 > 0 && runs.first(w - 1) <= pos - s0) {
+            // the second run of a unit says where all its parts are: the first in the run before, the others at the beginning of theirs
+            parts = runs.holding(pos - s0 + s.steps - 1) - w + 2;
+            if (tid == 0) {
+                merge[1] = s.q0 + row0;
+                merge[2] = rows;
+                merge[3] = kvh;
             }
-            merge[1] = parts;
         }
         pos += s1 - s0;
     }
+    if (tid == 0) merge[0] = parts;
 }
 
-// The parts of the units that runs have cut: workgroup (run, some of the columns) merges the unit whose second part is the first
-// of that run, in the order of the parts.
+// The parts of the units that runs have cut: workgroup (run, some of the columns) merges the unit that the run is the second to work
+// on, in the order of the parts.
 template <int HD>
-__global__ __launch_bounds__(kTreeThreads) void tree_merge_kernel(const TreeArgs p)
+__global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(const TreeArgs p)
 {
-    constexpr int COLS = 2 * kTreeThreads / HD;     // columns of a workgroup: a thread has two dims
+    constexpr int COLS = 4 * kMergeThreads / HD;    // columns of a workgroup: a thread has four dims
+    constexpr int AHEAD = 8;                        // parts whose loads are sent off together
     const int w = blockIdx.x;
     const int32_t *const merge = p.merges + (int64_t)w * kMergeInts;
-    const int parts = merge[1];
-    if (parts == 0) return;
-    const int second = merge[0], row0 = merge[2], rows = merge[3], kvh = merge[4];
-    const int col = blockIdx.y * COLS + threadIdx.x / (HD / 2), d = 2 * (threadIdx.x % (HD / 2));
-    const int row = col / p.g, head = col - row * p.g;
-    if (row >= rows) return;
-    auto slot_of = [&](int k) -> int64_t { return (2 * (int64_t)(w - 1 + k) + (k == 0 ? second : 0)) * kTreeCols + col; };
-    float M = -1e30f, l = 0.f, a0 = 0.f, a1 = 0.f;
-    for (int k = 0; k < parts; ++k) {
-        const int64_t slot = slot_of(k);
-        const f32x2 ml = *reinterpret_cast<const f32x2 *>(p.part_ml + 2 * slot);
-        const f32x2 a = *reinterpret_cast<const f32x2 *>(p.part_acc + slot * HD + d);
-        const float M_new = fmaxf(M, ml[0]);
-        const float w_old = fast_exp2(M - M_new), w_new = fast_exp2(ml[0] - M_new);
-        M = M_new;
-        l = l * w_old + ml[1] * w_new;
-        a0 = a0 * w_old + a[0] * w_new;
-        a1 = a1 * w_old + a[1] * w_new;
+    const int parts = merge[0], row0 = merge[1], rows = merge[2], kvh = merge[3];
+    const int d = 4 * (threadIdx.x % (HD / 4)), col = blockIdx.y * COLS + threadIdx.x / (HD / 4);
+    if (parts == 0 || col >= rows * p.g) return;
+    float M = -1e30f, l = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int k0 = 0; k0 < parts; k0 += AHEAD) {
+        f32x2 ml[AHEAD];
+        f32x4 a[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int part = min(k0 + k, parts - 1);
+            const int64_t at = (2 * (int64_t)(w - 1 + part) + (part == 0 ? 1 : 0)) * kTreeCols + col;
+            ml[k] = *reinterpret_cast<const f32x2 *>(p.part_ml + 2 * at);
+            a[k] = *reinterpret_cast<const f32x4 *>(p.part_acc + at * HD + d);
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            if (k0 + k >= parts) break;
+            const float M_new = fmaxf(M, ml[k][0]);
+            const float w_old = fast_exp2(M - M_new), w_new = fast_exp2(ml[k][0] - M_new);
+            M = M_new;
+            l = l * w_old + ml[k][1] * w_new;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] = acc[e] * w_old + a[k][e] * w_new;
+        }
     }
     const float inv = l == 0.f ? 0.f : 1.0f / l;
-    *reinterpret_cast<uint32_t *>(p.out + ((int64_t)(row0 + row) * p.Hq + kvh * p.g + head) * HD + d) = pack2_bf16(a0 * inv, a1 * inv);
+    const int row = col / p.g, head = col - row * p.g;
+    *reinterpret_cast<u32x2 *>(p.out + ((int64_t)(row0 + row) * p.Hq + kvh * p.g + head) * HD + d) =
+        u32x2{pack2_bf16(acc[0] * inv, acc[1] * inv), pack2_bf16(acc[2] * inv, acc[3] * inv)};
 }
 
 namespace {
@@ -537,16 +696,17 @@ int tree_runs_log2(int hd, int num_cus, size_t ws_bytes)
 hipError_t launch_attn_tree(TreeArgs &a, void *ws, hipStream_t s)
 {
     const unsigned runs = 1u << a.runs_log2;
+    a.tile_rows = kTreeCols / a.g;
     a.part_acc = static_cast<float *>(ws);
     a.part_ml = a.part_acc + (size_t)2 * runs * kTreeCols * a.hd;
     a.merges = reinterpret_cast<int32_t *>(a.part_ml + (size_t)2 * runs * kTreeCols * 2);
-    const dim3 merge_grid(runs, (unsigned)(kTreeCols * a.hd / (2 * kTreeThreads)));
+    const dim3 merge_grid(runs, (unsigned)(kTreeCols * a.hd / (4 * kMergeThreads)));
     if (a.hd == 128) {
         hipLaunchKernelGGL(tree_kernel<128>, dim3(runs), dim3(kTreeThreads), 0, s, a);
-        hipLaunchKernelGGL(tree_merge_kernel<128>, merge_grid, dim3(kTreeThreads), 0, s, a);
+        hipLaunchKernelGGL(tree_merge_kernel<128>, merge_grid, dim3(kMergeThreads), 0, s, a);
     } else {
         hipLaunchKernelGGL(tree_kernel<64>, dim3(runs), dim3(kTreeThreads), 0, s, a);
-        hipLaunchKernelGGL(tree_merge_kernel<64>, merge_grid, dim3(kTreeThreads), 0, s, a);
+        hipLaunchKernelGGL(tree_merge_kernel<64>, merge_grid, dim3(kMergeThreads), 0, s, a);
     }
     return hipGetLastError();
 }
