@@ -2148,7 +2148,8 @@ ooco_status ooco_attn_tree(ooco_ctx *ctx, const void *q, const void *k_cache, co
         if (!aligned(x, 16)) return fail(ctx, OOCO_EINVAL, "ooco_attn_tree: bf16 tensors must be 16-byte aligned");
     if (!aligned(masks, 8)) return fail(ctx, OOCO_EINVAL, "ooco_attn_tree: masks must be 8-byte aligned");
     TreeArgs a = {};
-    a.runs_log2 = tree_runs_log2(ctx->hd, ctx->num_cus, ctx->ws_bytes);
+    const int waves = tree_waves(total_q_tokens, num_seqs, ctx->g);
+    a.runs_log2 = tree_runs_log2(waves, ctx->hd, ctx->num_cus, ctx->ws_bytes);
     if (a.runs_log2 < 0) return fail(ctx, OOCO_ENOMEM, "ooco_attn_tree: the workspace (%zu bytes) holds no partial result", ctx->ws_bytes);
     a.q = static_cast<const uint16_t *>(q);
     a.k_cache = static_cast<const uint16_t *>(k_cache);
@@ -2170,7 +2171,7 @@ ooco_status ooco_attn_tree(ooco_ctx *ctx, const void *q, const void *k_cache, co
     a.scale_log2e = ctx->scale * 1.4426950408889634f;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     ctx->note_stream(s);
-    const hipError_t e = launch_attn_tree(a, ctx->ws, s);
+    const hipError_t e = launch_attn_tree(a, waves, ctx->ws, s);
     if (e != hipSuccess) return fail(ctx, OOCO_EHIP, "ooco_attn_tree: kernel launch: %s", hipGetErrorString(e));
     return OOCO_OK;
 }

@@ -19,7 +19,7 @@ struct TreeArgs {
     const int32_t *ctx_lens;
     const uint64_t *masks;      // [total_q][words]
     uint16_t *out;
-    int32_t *merges;            // [runs][4]: parts of the unit that the merge kernel has for the run, its first row, rows, kv head
+    int32_t *merges;            // [runs][5]: parts of the unit that the run continues (0: none), its first run, first row, rows, kv head
     float *part_acc;            // [2 * runs][columns of a tile][hd]  un-normalised partial outputs
     float *part_ml;             // [2 * runs][columns of a tile][2]   (reference in log2 units, sum)
     int64_t num_blocks;
@@ -28,12 +28,15 @@ struct TreeArgs {
     int32_t num_seqs, total_q, words;
     int32_t runs_log2;          // runs of the line: 1 << runs_log2 workgroups
     int32_t tile_rows;          // rows of the widest tile
+    int32_t short_line;         // up to 64 sequences, and a line of 31 bits
     float scale_log2e;          // softmax scale * log2(e)
 };
+// Waves of a workgroup: 4 or 8.
+int tree_waves(int total_q, int num_seqs, int g);
 // Runs (a power of two) that a workspace of ws_bytes allows on num_cus compute units, as their logarithm; < 0: none.
-int tree_runs_log2(int hd, int num_cus, size_t ws_bytes);
-// a.runs_log2 runs; the workspace pointers are set from ws.
-hipError_t launch_attn_tree(TreeArgs &a, void *ws, hipStream_t s);
+int tree_runs_log2(int waves, int hd, int num_cus, size_t ws_bytes);
+// a.runs_log2 runs; the workspace pointers and what follows from the waves are set here.
+hipError_t launch_attn_tree(TreeArgs &a, int waves, void *ws, hipStream_t s);
 
 // ---- masks and positions
 hipError_t launch_tree_masks(const int32_t *parents, const int32_t *query_start_loc, const int32_t *ctx_lens, uint64_t *masks,

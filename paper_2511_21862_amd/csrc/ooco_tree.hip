@@ -5,15 +5,16 @@
 // O^T[dim][query column] = V^T P^T; a query column is a (row, head of the GQA group) pair, so that the K and V of a token are
 // fetched once for all nodes and heads that see it.  One pass over the keys with the running maximum and sum of the softmax.
 //
-// Work: the columns of a sequence are cut into tiles of 128, the last as wide as 32, 64 or 128 columns have to be; each of a workgroup's
-// four waves has 32 columns, and the waves that columns leave over share the tokens.  Unit = (kv head, tile), walked in steps of 128
-// tokens.  The units of all sequences, steps end to end, form a line that is cut into equal runs, a workgroup each, two to a compute unit;
-// where a run ends inside a unit, partial results meet in the merge kernel.  The lengths are read and the line is laid out on the device by
-// every workgroup for itself: no plan and no host copy of lengths that the last step's verification has just decided.
-//   32 columns      every wave loads K and V of its own tokens from the cache to the registers of the matrix instructions: nothing is
-//                   shared, so nobody waits for anybody, and a compute unit has 128 KiB on their way
-//   64, 128         K and V of 64 tokens at a time go through LDS, for two or four waves, by direct loads into the other of two buffers
-//   128             the products of 32 tokens run beside the exponentials of 32 others (see region)
+// Work: the columns of a sequence are cut into tiles of 32 for each of the NW = 4 or 8 waves of a workgroup, the last tile as wide as 32, 64,
+// 128 or 256 columns have to be; the waves that columns leave over share the tokens.  Unit = (kv head, tile), walked in steps of 128
+// tokens.  The units of all sequences, steps end to end, form a line that is cut into equal runs, a workgroup each, two of four waves to a
+// compute unit or one of eight; where a run ends inside a unit, partial results meet in the merge kernel.  The lengths are read and the
+// line is laid out on the device by every workgroup for itself: no plan and no host copy of lengths that the last step's verification has
+// just decided.
+//   32 columns        every wave loads K and V of its own tokens from the cache to the registers of the matrix instructions: nothing is
+//                     shared, so nobody waits for anybody, and a compute unit has 128 KiB on their way
+//   more              K and V of 64 tokens at a time go through LDS by direct loads into the other of two buffers
+//   32 for each wave  the products of 32 tokens run beside the exponentials of 32 others (see region)
 #include "ooco_device.h"
 #include "ooco_internal.h"
 #include "ooco_spec.h"
@@ -23,12 +24,10 @@
 
 namespace ooco {
 
-constexpr int kTreeWaves = 4;
-constexpr int kTreeThreads = 64 * kTreeWaves;
-constexpr int kTreeCols = 32 * kTreeWaves;   // query columns of the widest tile
 constexpr int kTreeStep = 128;               // tokens of a step
 constexpr int kMinRun = 1;                   // steps of a run, at least
-constexpr int kMergeInts = 4;
+constexpr int kMergeInts = 5;
+constexpr int kMergeSlices = 8;
 constexpr int kMergeThreads = 256;
 
 // The largest of a lane's sixteen scores, NaN if one is.  (v_maximum3_f32, which needs no operand quieted.  Not the asm of max16:
@@ -45,9 +44,8 @@ OOCO_DEV float largest(const f32x16 &s)
 struct TreeSeq {
     int q0, n, ctx, len, steps;      // len: tokens that exist, the nodes among them
     int tile_rows, tiles;            // rows of a tile but the last
-    int last_waves;                  // waves that have columns of the last tile: 1, 2 or 4
+    int last_waves;                  // waves that have columns of the last tile: 1, 2, 4 or 8
     int64_t units;                   // steps of all its units
-    OOCO_DEV int unit_waves(int tile) const { return tile == tiles - 1 ? last_waves : kTreeWaves; }
 };
 OOCO_DEV TreeSeq tree_seq(const TreeArgs &p, int q0, int q1, int ctx)
 {
@@ -59,75 +57,16 @@ OOCO_DEV TreeSeq tree_seq(const TreeArgs &p, int q0, int q1, int ctx)
     s.ctx = min(max(ctx, 0), cap);
     s.len = (int)min((int64_t)s.ctx + min(s.n, 64 * p.words), (int64_t)cap);
     s.steps = (s.len + kTreeStep - 1) / kTreeStep;
-    s.tile_rows = p.tile_rows;       // (a group of heads that does not divide 128: the columns behind the last whole row are none)
+    s.tile_rows = p.tile_rows;       // (a group of heads that does not divide a tile: the columns behind the last whole row are none)
     s.tiles = (s.n + s.tile_rows - 1) / s.tile_rows;
     const int last_cols = (s.n - (s.tiles - 1) * s.tile_rows) * p.g;
-    s.last_waves = last_cols <= 32 ? 1 : last_cols <= 64 ? 2 : 4;
+    s.last_waves = last_cols <= 32 ? 1 : last_cols <= 64 ? 2 : last_cols <= 128 ? 4 : 8;
     s.units = (int64_t)s.tiles * p.Hkv * s.steps;
     return s;
 }
 // floor(a / b) of numbers below 2^53: a correctly rounded quotient does not reach the next integer.  (The compiler's 64-bit division
 // is some hundred instructions, and instructions are what a small launch waits for.)
 OOCO_DEV int64_t quotient(int64_t a, int64_t b) { return (int64_t)((double)a / (double)b); }
-
-// The line: its length, and the sequence that holds position `at(total)` of it, with the position of that sequence's first step.
-// All threads of the workgroup call it together.
-template <class At>
-OOCO_DEV int64_t tree_locate(const TreeArgs &p, At at, int &seq, int64_t &start)
-{
-    __shared__ int64_t wave_total[kTreeThreads / 64];
-    __shared__ int sh_seq;
-    __shared__ int64_t sh_start;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    auto units_of = [&](int i) -> int64_t {
-        return i < p.num_seqs ? tree_seq(p, p.query_start_loc[i], p.query_start_loc[i + 1], p.ctx_lens[i]).units : 0;
-    };
-    auto scan = [&](int64_t v, int64_t &all) -> int64_t {   // inclusive sum over the workgroup, and of all
-        int64_t x = v;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int64_t o = __shfl_up(x, d);
-            x += lane >= d ? o : 0;
-        }
-        __syncthreads();
-        if (lane == 63) wave_total[wave] = x;
-        __syncthreads();
-        all = 0;
-        int64_t before = 0;
-#pragma unroll
-        for (int w = 0; w < kTreeThreads / 64; ++w) {
-            before += w < wave ? wave_total[w] : 0;
-            all += wave_total[w];
-        }
-        return before + x;
-    };
-    int64_t total = 0, all, mine = 0, incl = 0;
-    for (int base = 0; base < p.num_seqs; base += kTreeThreads) {
-        mine = units_of(base + tid);
-        incl = scan(mine, all);
-        total += all;
-    }
-    const int64_t x = at(total);
-    int64_t before = 0;
-    for (int base = 0; base < p.num_seqs; base += kTreeThreads) {
-        if (p.num_seqs > kTreeThreads) {
-            mine = units_of(base + tid);
-            incl = scan(mine, all);
-        } else {
-            all = total;
-        }
-        if (before + incl - mine <= x && x < before + incl) {
-            sh_seq = base + tid;
-            sh_start = before + incl - mine;
-        }
-        before += all;
-        if (before > x) break;
-    }
-    __syncthreads();
-    seq = sh_seq;
-    start = sh_start;
-    return total;
-}
 
 // Values that are the same in every lane, in scalar registers.
 OOCO_DEV int64_t uniform(int64_t v)
@@ -153,6 +92,85 @@ struct TreeRuns {
     OOCO_DEV int64_t first(int w) const { return split ? (total * w) >> log2 : min(total, (int64_t)w * kMinRun); }
     OOCO_DEV int holding(int64_t x) const { return split ? (int)quotient(((x + 1) << log2) - 1, total) : (int)(x / kMinRun); }
 };
+
+// The line: its length, and the sequence that holds position at(total) of it, with the position of that sequence's first step.
+// All threads of the workgroup call it together.  Up to 64 sequences on a line of 31 bits: every wave looks them up for itself, a lane
+// each; the values that it needs next are then a lane away, and the next loads can go.
+template <int NT, class At>
+OOCO_DEV int64_t tree_locate(const TreeArgs &p, At at, int &seq, int64_t &start, TreeSeq &found)
+{
+    if (p.short_line) {
+        const int i = threadIdx.x & 63, j = min(i, p.num_seqs - 1);
+        const int q0 = p.query_start_loc[j], q1 = p.query_start_loc[j + 1], ctx = p.ctx_lens[j];
+        const int units = i < p.num_seqs ? (int)tree_seq(p, q0, q1, ctx).units : 0;
+        int incl = units;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(incl, d);
+            incl += i >= d ? o : 0;
+        }
+        const int total = __builtin_amdgcn_readlane(incl, 63);
+        const int64_t x = at((int64_t)total);
+        seq = min(__popcll(__ballot(incl <= x)), p.num_seqs - 1);
+        start = __builtin_amdgcn_readlane(incl - units, seq);
+        found = tree_seq(p, __builtin_amdgcn_readlane(q0, seq), __builtin_amdgcn_readlane(q1, seq), __builtin_amdgcn_readlane(ctx, seq));
+        return total;
+    }
+    __shared__ int64_t wave_total[NT / 64];
+    __shared__ int sh_seq;
+    __shared__ int64_t sh_start;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    auto units_of = [&](int i) -> int64_t {
+        return i < p.num_seqs ? tree_seq(p, p.query_start_loc[i], p.query_start_loc[i + 1], p.ctx_lens[i]).units : 0;
+    };
+    auto scan = [&](int64_t v, int64_t &all) -> int64_t {   // inclusive sum over the workgroup, and of all
+        int64_t x = v;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int64_t o = __shfl_up(x, d);
+            x += lane >= d ? o : 0;
+        }
+        __syncthreads();
+        if (lane == 63) wave_total[wave] = x;
+        __syncthreads();
+        all = 0;
+        int64_t before = 0;
+#pragma unroll
+        for (int w = 0; w < NT / 64; ++w) {
+            before += w < wave ? wave_total[w] : 0;
+            all += wave_total[w];
+        }
+        return before + x;
+    };
+    int64_t total = 0, all, mine = 0, incl = 0;
+    for (int base = 0; base < p.num_seqs; base += NT) {
+        mine = units_of(base + tid);
+        incl = scan(mine, all);
+        total += all;
+    }
+    const int64_t x = at(total);
+    int64_t before = 0;
+    for (int base = 0; base < p.num_seqs; base += NT) {
+        if (p.num_seqs > NT) {
+            mine = units_of(base + tid);
+            incl = scan(mine, all);
+        } else {
+            all = total;
+        }
+        if (before + incl - mine <= x && x < before + incl) {
+            sh_seq = base + tid;
+            sh_start = before + incl - mine;
+        }
+        before += all;
+        if (before > x) break;
+    }
+    __syncthreads();
+    if (x >= total) return uniform(total);
+    seq = __builtin_amdgcn_readfirstlane(sh_seq);
+    start = uniform(sh_start);
+    found = tree_seq_at(p, seq);
+    return uniform(total);
+}
 
 // What a wave does with 32 tokens, whichever way they come: its 32 query columns' share of the softmax and of the output.
 template <int HD>
@@ -246,43 +264,59 @@ struct TreeWave {
     }
 };
 
-// A tile of K or of V (one block, one kv head) from the cache into LDS, HD / 32 loads of 16 bytes per lane: 1 KiB each, contiguous in LDS
-// from dst on.  off[n]: the lane's place in the tile for load n, less n KiB (the instruction's offset counts for both addresses).
-template <int HD>
-OOCO_DEV void tile_to_lds(const char *base, uint32_t dst, const uint32_t (&off)[4])
+// A wave's share of the loads of a tile of K or of V (one block, one kv head) from the cache into LDS: NL loads of 16 bytes per lane, 1 KiB each,
+// contiguous in LDS from dst on.  off[n]: the lane's place in the tile for load n, less n KiB (the instruction's offset counts for both
+// addresses).  once: nobody else reads the tile, so it need not push anything out of the caches (64 sequences of 16 nodes on 4096 tokens,
+// 32/8 heads, us: 197 -> 177).
+template <int NL>
+OOCO_DEV void tile_to_lds(const char *base, uint32_t dst, const uint32_t (&off)[NL], bool once)
 {
     uint32_t saved_m0;   // M0 is restored: the compiler may keep a value of its own there
-    if constexpr (HD == 128)
-        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
-                     "global_load_lds_dwordx4 %2, %6\n\tglobal_load_lds_dwordx4 %3, %6 offset:1024\n\t"
-                     "global_load_lds_dwordx4 %4, %6 offset:2048\n\tglobal_load_lds_dwordx4 %5, %6 offset:3072\n\ts_mov_b32 m0, %0"
-                     : "=&s"(saved_m0)
-                     : "s"(dst), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(base)
-                     : "memory");
-    else
-        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
-                     "global_load_lds_dwordx4 %2, %4\n\tglobal_load_lds_dwordx4 %3, %4 offset:1024\n\ts_mov_b32 m0, %0"
-                     : "=&s"(saved_m0)
-                     : "s"(dst), "v"(off[0]), "v"(off[1]), "s"(base)
-                     : "memory");
+#define OOCO_ASM(loads, ...) \
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t" loads "s_mov_b32 m0, %0" : "=&s"(saved_m0) : "s"(dst), "s"(base), __VA_ARGS__ : "memory")
+#define OOCO_LOAD(v, at, nt) "global_load_lds_dwordx4 " v ", %2 offset:" at nt "\n\t"
+    if constexpr (NL == 4) {
+        if (once)
+            OOCO_ASM(OOCO_LOAD("%3", "0", " nt") OOCO_LOAD("%4", "1024", " nt") OOCO_LOAD("%5", "2048", " nt") OOCO_LOAD("%6", "3072", " nt"),
+                     "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]));
+        else
+            OOCO_ASM(OOCO_LOAD("%3", "0", "") OOCO_LOAD("%4", "1024", "") OOCO_LOAD("%5", "2048", "") OOCO_LOAD("%6", "3072", ""),
+                     "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]));
+    } else if constexpr (NL == 2) {
+        if (once)
+            OOCO_ASM(OOCO_LOAD("%3", "0", " nt") OOCO_LOAD("%4", "1024", " nt"), "v"(off[0]), "v"(off[1]));
+        else
+            OOCO_ASM(OOCO_LOAD("%3", "0", "") OOCO_LOAD("%4", "1024", ""), "v"(off[0]), "v"(off[1]));
+    } else {
+        static_assert(NL == 1, "loads of a wave");
+        if (once)
+            OOCO_ASM(OOCO_LOAD("%3", "0", " nt"), "v"(off[0]));
+        else
+            OOCO_ASM(OOCO_LOAD("%3", "0", ""), "v"(off[0]));
+    }
+#undef OOCO_ASM
+#undef OOCO_LOAD
 }
 
 constexpr int kStageTokens = 64;                              // tokens that go through LDS at a time
-constexpr int kStageBlocks = kStageTokens / kBlockSize;       // a block for each wave to bring
-static_assert(kStageBlocks == kTreeWaves && kTreeStep % kStageTokens == 0, "stages of a step");
+constexpr int kStageBlocks = kStageTokens / kBlockSize;       // a block for each of four waves to bring, or half a block for each of eight
+static_assert(kTreeStep == 2 * kStageTokens, "stages of a step");
 
-template <int HD>
-__global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(const TreeArgs p)
+template <int HD, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void tree_kernel(const TreeArgs p)
 {
+    constexpr int NT = 64 * NW, COLS = 32 * NW;
+    constexpr int SHARE = NW / kStageBlocks;      // waves that bring a block
+    constexpr int NL = HD / 32 / SHARE;           // loads of a wave for its share of a tile
     using Wave = TreeWave<HD>;
     constexpr int KS = Wave::KS, MB = Wave::MB;
     constexpr int ROW = HD + 4;                   // floats of a column in LDS (padded: the lanes of a wave are columns)
     constexpr int CH = 2 * HD;                    // 16-byte pieces of a tile of K or V
     constexpr int STAGE = kStageBlocks * CH;
     constexpr int64_t kTile = (int64_t)HD * kBlockSize;
-    constexpr int kSlab = kTreeWaves * 32 * ROW * 4, kStage = 2 * 2 * STAGE * 16;
+    constexpr int kSlab = NW * 32 * ROW * 4, kStage = 2 * 2 * STAGE * 16;
     __shared__ __align__(16) unsigned char lds[kSlab > kStage ? kSlab : kStage];
-    __shared__ float stat[kTreeWaves][32][2];
+    __shared__ float stat[NW][32][2];
     float (*const slab)[32][ROW] = reinterpret_cast<float (*)[32][ROW]>(lds);           // [wave][column][dim]
     u32x4 *const ldsK = reinterpret_cast<u32x4 *>(lds), *const ldsV = ldsK + 2 * STAGE;   // [buffer][block][piece]
 
@@ -291,13 +325,19 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(const TreeArgs p)
     const int col = lane & 31, h = lane >> 5;
     const int g = p.g;
     // Runs next to each other on the line are on one XCD (workgroup b runs on XCD b % 8): the tiles of one sequence and kv head walk the
-    // same tokens at about the same time, and share an L2.
-    const int w = p.runs_log2 >= 3 ? (int)((blockIdx.x & 7) << (p.runs_log2 - 3)) + (int)(blockIdx.x >> 3) : (int)blockIdx.x;
-
-    int seq = 0;
+    // same tokens at about the same time, and share an L2 (512 columns on 14,000 tokens, us: 286 -> 255).  A line of fewer runs than there
+    // are workgroups is spread over the XCDs.
+    int w = blockIdx.x, seq = 0;
     int64_t start = 0;
-    const int64_t total = uniform(tree_locate(p, [&](int64_t t) { return TreeRuns(t, p.runs_log2).first(w); }, seq, start));
-    start = uniform(start);
+    TreeSeq s = {};
+    const int64_t total = tree_locate<NT>(
+        p,
+        [&](int64_t t) {
+            const TreeRuns r(t, p.runs_log2);
+            if (r.split && p.runs_log2 >= 3) w = (int)((blockIdx.x & 7) << (p.runs_log2 - 3)) + (int)(blockIdx.x >> 3);
+            return r.first(w);
+        },
+        seq, start, s);
     const TreeRuns runs(total, p.runs_log2);
     const int64_t lo = runs.first(w), hi = runs.first(w + 1);
     int32_t *const merge = p.merges + (int64_t)w * kMergeInts;
@@ -308,22 +348,22 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(const TreeArgs p)
     // K operand row col -> block (col >> 4) of the 32 tokens, slot with bits 2 and 3 swapped, so that register r of S^T is token
     // 16 (r / 8) + 8 h + r % 8: eight consecutive tokens of a block, as a 16-byte piece of V has them
     const int ku = col >> 4, kslot = (col & 3) | ((col & 4) << 1) | ((col & 8) >> 1);
-    // Pieces of a tile in LDS: K as in the cache, V [half of the tokens][dim], so that the lanes that read together read side by side
+    // Pieces of a tile in LDS: K as in the cache, V [half of the tokens][dim], so that the lanes that read together read side by side.  Where
+    // this wave's share of a tile comes from:
     constexpr int kBias = 4096;   // (keeps the offsets of V positive)
-    uint32_t k_off[4], v_off[4];
+    const int share = (wave & (SHARE - 1)) * NL * 64;   // first piece
+    uint32_t k_off[NL], v_off[NL];
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
-        const int c = 64 * n + lane;
-        k_off[n] = (uint32_t)lane * 16u;
+    for (int n = 0; n < NL; ++n) {
+        const int c = share + 64 * n + lane;
+        k_off[n] = (uint32_t)(share + lane) * 16u;
         v_off[n] = (uint32_t)((2 * (c % HD) + c / HD) * 16 - n * 1024 + kBias);
     }
     const uint32_t ldsK_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)ldsK;
     const uint32_t ldsV_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)ldsV;
 
     int64_t pos = lo;
-    int parts = 0;   // of the unit that the run begins inside of, if the run is the second that works on it
-    seq = __builtin_amdgcn_readfirstlane(seq);
-    TreeSeq s = tree_seq_at(p, seq);
+    int parts = 0, first_run = 0;   // of the unit that the run begins inside of
     while (pos < hi) {
         while (pos - start >= s.units) {   // the next sequence with rows
             start += s.units;
@@ -334,7 +374,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(const TreeArgs p)
         const int s0 = (int)(pos - start - (int64_t)unit * s.steps);
         const int s1 = (int)min((int64_t)s.steps, s0 + (hi - pos));
         const int kvh = s.tiles == 1 ? unit : unit / s.tiles, tile = unit - kvh * s.tiles;
-        const int waves = s.unit_waves(tile);
+        const int waves = tile == s.tiles - 1 ? s.last_waves : NW;
         const int row0 = tile * s.tile_rows, rows = min(s.tile_rows, s.n - row0);
 
         const int cw = wave & (waves - 1), kw = wave / waves;   // this wave's columns, and its share of the tokens
@@ -351,13 +391,13 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(const TreeArgs p)
         Wave x;
         __syncthreads();   // (LDS: the last unit's results have been read)
         if (waves == 1) {
-            // 32 tokens, two blocks, at a time: those of the run from 32 * wave on, every 128.  Loads behind the wave's last tokens fetch
+            // 32 tokens, two blocks, at a time: those of the run from 32 * wave on, every 32 * NW.  Loads behind the wave's last tokens fetch
             // those again, so that every turn has the same number of loads on their way.
             const int t_end = min(4 * s1, (s.len + 31) / 32);
             int t = 4 * s0 + wave;
             x.begin(p, q_row, kvh * g + c_head, h);
             if (t < t_end) {
-                const int t_last = t + (t_end - 1 - t) / kTreeWaves * kTreeWaves;
+                const int t_last = t + (t_end - 1 - t) / NW * NW;
                 int ida = id_at(2 * t), idb = id_at(2 * t + 1);
                 u32x4 kr[KS], vr[2][MB];
                 int64_t at0, at1;
@@ -383,8 +423,8 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(const TreeArgs p)
                 load_k();
                 __builtin_amdgcn_sched_barrier(kNoVmem);   // (the scores wait for K alone)
                 load_v();
-                next_ids(t + kTreeWaves);
-                for (; t < t_end; t += kTreeWaves) {
+                next_ids(t + NW);
+                for (; t < t_end; t += NW) {
                     const int tok0 = 32 * t, left = s.len - tok0;
                     f32x16 S;
 #pragma unroll
@@ -415,16 +455,18 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(const TreeArgs p)
                             x.O[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vr[b][mb]), __builtin_bit_cast(bf16x8, P[b]),
                                                                               x.O[mb], 0, 0, 0);
                     load_v();
-                    next_ids(t + 2 * kTreeWaves);
+                    next_ids(t + 2 * NW);
                 }
             }
         } else {
-            // Stages of 64 tokens, f0 .. f1 - 1 (the sequence's last step may have one); wave i brings block i of a stage.
+            // Stages of 64 tokens, f0 .. f1 - 1 (the sequence's last step may have one); a wave brings a block of a stage, or half of one.
             const int f0 = 2 * s0, f1 = min(2 * s1, (s.len + kStageTokens - 1) / kStageTokens);
-            auto stage_id = [&](int f) -> int { return id_at(kStageBlocks * f + wave); };
-            auto stage_k = [&](int f, int id) { tile_to_lds<HD>(k_cache + bytes_at(id), ldsK_at + (uint32_t)((f & 1) * STAGE + wave * CH) * 16u, k_off); };
+            const bool once = s.tiles == 1;
+            auto stage_id = [&](int f) -> int { return id_at(kStageBlocks * f + wave / SHARE); };
+            const uint32_t to = (uint32_t)(wave / SHARE * CH + share) * 16u;
+            auto stage_k = [&](int f, int id) { tile_to_lds(k_cache + bytes_at(id), ldsK_at + (uint32_t)((f & 1) * STAGE) * 16u + to, k_off, once); };
             auto stage_v = [&](int f, int id) {
-                tile_to_lds<HD>(v_cache + bytes_at(id) - kBias, ldsV_at + (uint32_t)((f & 1) * STAGE + wave * CH) * 16u, v_off);
+                tile_to_lds(v_cache + bytes_at(id) - kBias, ldsV_at + (uint32_t)((f & 1) * STAGE) * 16u + to, v_off, once);
             };
             // Everybody's loads have landed, and everybody is done with what came before; V of stage f is used next.
             auto arrive = [&](int f) {
@@ -432,7 +474,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(const TreeArgs p)
                 __syncthreads();
                 if (kStageTokens * (f + 1) > s.len) {   // (slots past the end may hold anything, and 0 * NaN is NaN)
                     u32x4 *const V = ldsV + (f & 1) * STAGE;
-                    for (int i = tid; i < STAGE; i += kTreeThreads) {
+                    for (int i = tid; i < STAGE; i += NT) {
                         const int first = kStageTokens * f + 16 * (i / CH) + 8 * (i % CH / HD);
                         u32x4 keep;
 #pragma unroll
@@ -446,13 +488,13 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(const TreeArgs p)
             // operand i of the product of 32 tokens (half a stage) with K and of their weights with V
             auto k_operand = [&](int f, int half, int i) -> u32x4 { return ldsK[(f & 1) * STAGE + (2 * half + ku) * CH + (2 * i + h) * kBlockSize + kslot]; };
             auto v_operand = [&](int f, int half, int i) -> u32x4 { return ldsV[(f & 1) * STAGE + (2 * half + i / MB) * CH + h * HD + 32 * (i % MB) + col]; };
-            const bool used = 32 * cw < rows * g;   // (columns behind the last row: such waves only bring blocks)
+            const bool used = 32 * cw < rows * g && kw < 2;   // (waves without columns, or without tokens, only bring blocks)
             int id0 = stage_id(f0), id1 = stage_id(f0 + 1);
             stage_k(f0, id0);
             stage_v(f0, id0);
-            if (waves == 2) {
+            if (waves < NW) {
                 x.begin(p, q_row, kvh * g + c_head, h);
-                for (int f = f0; f < f1; ++f) {   // a half stage for each of the two waves that have the same columns
+                for (int f = f0; f < f1; ++f) {   // half a stage for each of two waves that have the same columns
                     arrive(f);
                     if (f + 1 < f1) {
                         stage_k(f + 1, id1);
@@ -587,20 +629,20 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(const TreeArgs p)
                 *reinterpret_cast<f32x4 *>(&slab[wave][col][32 * mb + 8 * k + 4 * h]) =
                     f32x4{x.O[mb][4 * k], x.O[mb][4 * k + 1], x.O[mb][4 * k + 2], x.O[mb][4 * k + 3]};
         __syncthreads();
-        constexpr int PER = HD / 8;               // dims of a thread: eight threads have a column
+        constexpr int TC = NT / 32, PER = HD / TC;   // threads of a column, dims of each
         const bool whole = s0 == 0 && s1 == s.steps;
         const int64_t slot = 2 * (int64_t)w + (s0 == 0 ? 1 : 0);   // (a run has one unit that begins before it, and one that ends behind it)
         for (int i = 0; i < waves; ++i) {
-            const int oc = 32 * i + tid / 8, od = (tid & 7) * PER;
+            const int oc = 32 * i + tid / TC, od = (tid % TC) * PER;
             const int o_row = oc / g, o_head = oc - o_row * g;
             if (o_row >= rows) break;
             float M = -INFINITY;
-            for (int k = i; k < kTreeWaves; k += waves) M = fmaxf(M, stat[k][oc & 31][0]);
+            for (int k = i; k < NW; k += waves) M = fmaxf(M, stat[k][oc & 31][0]);
             float l = 0.f;
             f32x4 acc[PER / 4];
 #pragma unroll
             for (int j = 0; j < PER / 4; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-            for (int k = i; k < kTreeWaves; k += waves) {
+            for (int k = i; k < NW; k += waves) {
                 const float weight = fast_exp2(stat[k][oc & 31][0] - M);
                 l += stat[k][oc & 31][1] * weight;
 #pragma unroll
@@ -617,98 +659,131 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_kernel(const TreeArgs p)
                 for (int j = 0; j < PER / 4; ++j)
                     op[j] = u32x2{pack2_bf16(acc[j][0] * inv, acc[j][1] * inv), pack2_bf16(acc[j][2] * inv, acc[j][3] * inv)};
             } else {
-                f32x4 *const ap = reinterpret_cast<f32x4 *>(p.part_acc + (slot * kTreeCols + oc) * HD + od);
+                f32x4 *const ap = reinterpret_cast<f32x4 *>(p.part_acc + (slot * COLS + oc) * HD + od);
 #pragma unroll
                 for (int j = 0; j < PER / 4; ++j) ap[j] = acc[j];
-                if ((tid & 7) == 0) {
-                    p.part_ml[(slot * kTreeCols + oc) * 2] = M;
-                    p.part_ml[(slot * kTreeCols + oc) * 2 + 1] = l;
+                if (tid % TC == 0) {
+                    p.part_ml[(slot * COLS + oc) * 2] = M;
+                    p.part_ml[(slot * COLS + oc) * 2 + 1] = l;
                 }
             }
         }
-        if (s0 > 0 && runs.first(w - 1) <= pos - s0) {
-            // the second run of a unit says where all its parts are: the first in the run before, the others at the beginning of theirs
-            parts = runs.holding(pos - s0 + s.steps - 1) - w + 2;
+        if (s0 > 0) {   // (at most once, at the beginning of the run)
+            // where all parts of the unit are: the first in the run that the unit begins in, the others at the beginnings of theirs
+            first_run = runs.holding(pos - s0);
+            parts = runs.holding(pos - s0 + s.steps - 1) - first_run + 1;
             if (tid == 0) {
-                merge[1] = s.q0 + row0;
-                merge[2] = rows;
-                merge[3] = kvh;
+                merge[2] = s.q0 + row0;
+                merge[3] = rows;
+                merge[4] = kvh;
             }
         }
         pos += s1 - s0;
     }
-    if (tid == 0) merge[0] = parts;
+    if (tid == 0) {
+        merge[0] = parts;
+        merge[1] = first_run;
+    }
 }
 
-// The parts of the units that runs have cut: workgroup (run, some of the columns) merges the unit that the run is the second to work
-// on, in the order of the parts.
-template <int HD>
+// The parts of the units that runs have cut.  Every run that continues a unit takes a share of its columns, so that a unit of many
+// parts, which has many runs, is merged by many workgroups; kMergeSlices of them have the run's share.  In a workgroup HD / 4 threads
+// have a column's dims, and groups of threads have every PG-th part of it; their results meet in LDS in a fixed order.
+template <int HD, int NW>
 __global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(const TreeArgs p)
 {
-    constexpr int COLS = 4 * kMergeThreads / HD;    // columns of a workgroup: a thread has four dims
-    constexpr int AHEAD = 8;                        // parts whose loads are sent off together
+    constexpr int TC = HD / 4, SLOTS = kMergeThreads / TC;   // threads of a column, columns or groups at a time
+    constexpr int AHEAD = 4;                                 // parts whose loads are sent off together
+    __shared__ f32x4 sh_acc[kMergeThreads];
+    __shared__ f32x2 sh_ml[kMergeThreads];
     const int w = blockIdx.x;
     const int32_t *const merge = p.merges + (int64_t)w * kMergeInts;
-    const int parts = merge[0], row0 = merge[1], rows = merge[2], kvh = merge[3];
-    const int d = 4 * (threadIdx.x % (HD / 4)), col = blockIdx.y * COLS + threadIdx.x / (HD / 4);
-    if (parts == 0 || col >= rows * p.g) return;
-    float M = -1e30f, l = 0.f;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int k0 = 0; k0 < parts; k0 += AHEAD) {
-        f32x2 ml[AHEAD];
-        f32x4 a[AHEAD];
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            const int part = min(k0 + k, parts - 1);
-            const int64_t at = (2 * (int64_t)(w - 1 + part) + (part == 0 ? 1 : 0)) * kTreeCols + col;
-            ml[k] = *reinterpret_cast<const f32x2 *>(p.part_ml + 2 * at);
-            a[k] = *reinterpret_cast<const f32x4 *>(p.part_acc + at * HD + d);
-        }
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            if (k0 + k >= parts) break;
-            const float M_new = fmaxf(M, ml[k][0]);
-            const float w_old = fast_exp2(M - M_new), w_new = fast_exp2(ml[k][0] - M_new);
+    const int parts = merge[0], first = merge[1], row0 = merge[2], rows = merge[3], kvh = merge[4];
+    if (parts == 0) return;
+    const int cols = rows * p.g, shares = (parts - 1) * kMergeSlices, share = (w - first - 1) * kMergeSlices + blockIdx.y;
+    const int c0 = cols * share / shares, c1 = cols * (share + 1) / shares;
+    const int groups = parts <= AHEAD ? 1 : parts <= 2 * AHEAD ? 2 : parts <= 4 * AHEAD ? 4 : SLOTS;
+    const int slot = threadIdx.x / TC, d = 4 * (threadIdx.x % TC);
+    const int group = slot & (groups - 1);
+    for (int base = c0; base < c1; base += SLOTS / groups) {
+        const int col = base + slot / groups;
+        float M = -1e30f, l = 0.f;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        auto fold = [&](float m2, float l2, const f32x4 &a2) {
+            const float M_new = fmaxf(M, m2);
+            const float w_old = fast_exp2(M - M_new), w_new = fast_exp2(m2 - M_new);
             M = M_new;
-            l = l * w_old + ml[k][1] * w_new;
+            l = l * w_old + l2 * w_new;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[e] = acc[e] * w_old + a[k][e] * w_new;
+            for (int e = 0; e < 4; ++e) acc[e] = acc[e] * w_old + a2[e] * w_new;
+        };
+        if (col < c1) {
+            for (int k0 = group; k0 < parts; k0 += AHEAD * groups) {
+                f32x2 ml[AHEAD];
+                f32x4 a[AHEAD];
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) {
+                    const int k = k0 + i * groups;
+                    if (k < parts) {
+                        const int64_t at = (2 * (int64_t)(first + k) + (k == 0 ? 1 : 0)) * (32 * NW) + col;
+                        ml[i] = *reinterpret_cast<const f32x2 *>(p.part_ml + 2 * at);
+                        a[i] = *reinterpret_cast<const f32x4 *>(p.part_acc + at * HD + d);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i)
+                    if (k0 + i * groups < parts) fold(ml[i][0], ml[i][1], a[i]);
+            }
+        }
+        __syncthreads();   // (the last columns' results have been read)
+        sh_acc[threadIdx.x] = acc;
+        sh_ml[threadIdx.x] = f32x2{M, l};
+        __syncthreads();
+        if (group == 0 && col < c1) {
+            for (int k = 1; k < groups; ++k) fold(sh_ml[threadIdx.x + k * TC][0], sh_ml[threadIdx.x + k * TC][1], sh_acc[threadIdx.x + k * TC]);
+            const float inv = l == 0.f ? 0.f : 1.0f / l;
+            const int row = col / p.g, head = col - row * p.g;
+            *reinterpret_cast<u32x2 *>(p.out + ((int64_t)(row0 + row) * p.Hq + kvh * p.g + head) * HD + d) =
+                u32x2{pack2_bf16(acc[0] * inv, acc[1] * inv), pack2_bf16(acc[2] * inv, acc[3] * inv)};
         }
     }
-    const float inv = l == 0.f ? 0.f : 1.0f / l;
-    const int row = col / p.g, head = col - row * p.g;
-    *reinterpret_cast<u32x2 *>(p.out + ((int64_t)(row0 + row) * p.Hq + kvh * p.g + head) * HD + d) =
-        u32x2{pack2_bf16(acc[0] * inv, acc[1] * inv), pack2_bf16(acc[2] * inv, acc[3] * inv)};
 }
 
 namespace {
-size_t run_bytes(int hd) { return kMergeInts * sizeof(int32_t) + 2 * (size_t)kTreeCols * (hd + 2) * sizeof(float); }
+size_t run_bytes(int hd, int waves) { return kMergeInts * sizeof(int32_t) + 2 * (size_t)(32 * waves) * (hd + 2) * sizeof(float); }
+
+template <int HD, int NW>
+hipError_t launch(TreeArgs &a, void *ws, hipStream_t s)
+{
+    const unsigned runs = 1u << a.runs_log2;
+    a.tile_rows = 32 * NW / a.g;
+    const int64_t tiles = a.total_q / a.tile_rows + (int64_t)a.num_seqs, steps = (int64_t)a.max_blocks_per_seq * kBlockSize / kTreeStep + 1;
+    a.short_line = a.num_seqs <= 64 && (double)tiles * (double)a.Hkv * (double)steps < 2147483647.0;
+    a.part_acc = static_cast<float *>(ws);
+    a.part_ml = a.part_acc + (size_t)2 * runs * (32 * NW) * HD;
+    a.merges = reinterpret_cast<int32_t *>(a.part_ml + (size_t)2 * runs * (32 * NW) * 2);
+    hipLaunchKernelGGL((tree_kernel<HD, NW>), dim3(runs), dim3(64 * NW), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((tree_merge_kernel<HD, NW>), dim3(runs, kMergeSlices), dim3(kMergeThreads), 0, s, a);
+    return hipGetLastError();
+}
 }  // namespace
 
-int tree_runs_log2(int hd, int num_cus, size_t ws_bytes)
+int tree_waves(int total_q, int num_seqs, int g) { return (int64_t)total_q * g > 128 * (int64_t)num_seqs ? 8 : 4; }
+
+int tree_runs_log2(int waves, int hd, int num_cus, size_t ws_bytes)
 {
     int log2 = 0;
-    while ((2 << log2) <= 2 * num_cus) ++log2;   // two workgroups per compute unit
-    while (log2 >= 0 && (run_bytes(hd) << log2) > ws_bytes) --log2;
+    while ((2 << log2) <= 8 / waves * num_cus) ++log2;   // eight waves to a compute unit
+    while (log2 >= 0 && (run_bytes(hd, waves) << log2) > ws_bytes) --log2;
     return log2;
 }
 
-hipError_t launch_attn_tree(TreeArgs &a, void *ws, hipStream_t s)
+hipError_t launch_attn_tree(TreeArgs &a, int waves, void *ws, hipStream_t s)
 {
-    const unsigned runs = 1u << a.runs_log2;
-    a.tile_rows = kTreeCols / a.g;
-    a.part_acc = static_cast<float *>(ws);
-    a.part_ml = a.part_acc + (size_t)2 * runs * kTreeCols * a.hd;
-    a.merges = reinterpret_cast<int32_t *>(a.part_ml + (size_t)2 * runs * kTreeCols * 2);
-    const dim3 merge_grid(runs, (unsigned)(kTreeCols * a.hd / (4 * kMergeThreads)));
-    if (a.hd == 128) {
-        hipLaunchKernelGGL(tree_kernel<128>, dim3(runs), dim3(kTreeThreads), 0, s, a);
-        hipLaunchKernelGGL(tree_merge_kernel<128>, merge_grid, dim3(kMergeThreads), 0, s, a);
-    } else {
-        hipLaunchKernelGGL(tree_kernel<64>, dim3(runs), dim3(kTreeThreads), 0, s, a);
-        hipLaunchKernelGGL(tree_merge_kernel<64>, merge_grid, dim3(kMergeThreads), 0, s, a);
-    }
-    return hipGetLastError();
+    if (a.hd == 128) return waves == 8 ? launch<128, 8>(a, ws, s) : launch<128, 4>(a, ws, s);
+    return waves == 8 ? launch<64, 8>(a, ws, s) : launch<64, 4>(a, ws, s);
 }
 
 }  // namespace ooco
