@@ -507,7 +507,7 @@ ooco_status ooco_attn_tree(ooco_ctx *ctx, const void *q /*DEVICE*/, const void *
  * nodes, or if nothing is left): the first token whose running sum exceeds final_uniforms[i] times the whole sum (or, where rounding
  * leaves none, the last one that has any weight).  Tokens drawn so are distributed as the target's, whatever the draft.
  *   target_probs, draft_probs: DEVICE, fp32 (bf16_probs == 0) or bf16, rows row_stride >= vocab elements apart, aligned to their
- *     element; values that are not finite, or negative, have no weight
+ *     element; values that are not finite, or negative, have no weight.  1 <= vocab <= 2^30
  *   tokens: DEVICE int32 [total_q_tokens] (the root's is not looked at; one outside [0, vocab) is never accepted)
  *   parents: DEVICE int32 [total_q_tokens] as for ooco_tree_masks, or NULL: chains, the parent of node t is t - 1.  Trees with
  *     draft_probs are refused (OOCO_EINVAL).

@@ -2148,7 +2148,7 @@ ooco_status ooco_attn_tree(ooco_ctx *ctx, const void *q, const void *k_cache, co
         if (!aligned(x, 16)) return fail(ctx, OOCO_EINVAL, "ooco_attn_tree: bf16 tensors must be 16-byte aligned");
     if (!aligned(masks, 8)) return fail(ctx, OOCO_EINVAL, "ooco_attn_tree: masks must be 8-byte aligned");
     TreeArgs a = {};
-    const int waves = tree_waves(total_q_tokens, num_seqs, ctx->g);
+    const int waves = tree_waves(total_q_tokens, num_seqs, ctx->Hkv, ctx->g, ctx->max_blocks_per_seq, ctx->num_cus);
     a.runs_log2 = tree_runs_log2(waves, ctx->hd, ctx->num_cus, ctx->ws_bytes);
     if (a.runs_log2 < 0) return fail(ctx, OOCO_ENOMEM, "ooco_attn_tree: the workspace (%zu bytes) holds no partial result", ctx->ws_bytes);
     a.q = static_cast<const uint16_t *>(q);
@@ -2182,7 +2182,7 @@ ooco_status ooco_verify_drafts(ooco_ctx *ctx, const void *target_probs, const vo
                                int num_seqs, int total_q_tokens, void *stream)
 {
     if (!ctx) return OOCO_EINVAL;
-    if (vocab <= 0 || row_stride < vocab || max_path < 0)
+    if (vocab <= 0 || vocab > 1 << 30 || row_stride < vocab || max_path < 0)
         return fail(ctx, OOCO_EINVAL, "ooco_verify_drafts: vocab=%d row_stride=%lld max_path=%d", vocab, (long long)row_stride, max_path);
     if (parents && draft_probs) return fail(ctx, OOCO_EINVAL, "ooco_verify_drafts: draft_probs are for chains (parents == NULL)");
     ooco_status st;
@@ -2210,10 +2210,10 @@ ooco_status ooco_verify_drafts(ooco_ctx *ctx, const void *target_probs, const vo
     a.max_path = max_path;
     a.num_seqs = num_seqs;
     a.total_q = total_q_tokens;
-    verify_chunks(a, ctx->num_cus);
+    verify_layout(a, bf16_probs != 0, ctx->num_cus);
     if (verify_workspace(a) > ctx->ws_bytes)
         return fail(ctx, OOCO_ENOMEM, "ooco_verify_drafts: the sums take %zu bytes of workspace, there are %zu", verify_workspace(a), ctx->ws_bytes);
-    if ((int64_t)num_seqs * a.chunks > INT32_MAX) return fail(ctx, OOCO_ENOMEM, "ooco_verify_drafts: %d sequences of %d pieces", num_seqs, a.chunks);
+    if ((int64_t)num_seqs * a.groups > INT32_MAX) return fail(ctx, OOCO_ENOMEM, "ooco_verify_drafts: %d sequences of %d workgroups", num_seqs, a.groups);
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     ctx->note_stream(s);
     const hipError_t e = launch_verify(a, bf16_probs != 0, s);

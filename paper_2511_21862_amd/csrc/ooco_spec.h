@@ -32,7 +32,7 @@ struct TreeArgs {
     float scale_log2e;          // softmax scale * log2(e)
 };
 // Waves of a workgroup: 4 or 8.
-int tree_waves(int total_q, int num_seqs, int g);
+int tree_waves(int total_q, int num_seqs, int Hkv, int g, int max_blocks_per_seq, int num_cus);
 // Runs (a power of two) that a workspace of ws_bytes allows on num_cus compute units, as their logarithm; < 0: none.
 int tree_runs_log2(int waves, int hd, int num_cus, size_t ws_bytes);
 // a.runs_log2 runs; the workspace pointers and what follows from the waves are set here.
@@ -72,16 +72,16 @@ struct VerifyArgs {
     const float *final_uniforms;         // [num_seqs]
     const int32_t *query_start_loc;
     int32_t *counts, *path, *out_tokens;
-    double *sums;                        // [num_seqs][chunks][2]
+    double *sums;                        // [num_seqs][pieces of a row][2]: what is left, and what there was
     int32_t *arrivals;                   // [num_seqs], zero between calls
     int64_t stride;
     int32_t vocab, max_path;
     int32_t num_seqs, total_q;
-    int32_t chunk, chunks;               // elements of a row that a workgroup sums, and such pieces of a row
+    int32_t pieces, groups;              // pieces of a row that a wave sums, and workgroups that share a row
 };
 constexpr int kMaxVerifyNodes = 256;
 size_t verify_workspace(const VerifyArgs &a);
-void verify_chunks(VerifyArgs &a, int num_cus);
+void verify_layout(VerifyArgs &a, bool bf16, int num_cus);
 hipError_t launch_verify(const VerifyArgs &a, bool bf16, hipStream_t s);
 
 // ---- accepted nodes to their places

@@ -223,12 +223,15 @@ hipError_t launch_rope_append(RopeArgs &a, bool interleaved, int num_cus, hipStr
 // (draft == NULL).  The first accepted child of each node is all that the walk from the root needs, and whether a child is
 // accepted does not depend on the walk: one thread per node tests its own, after one round of gathered loads.  The token behind
 // the last accepted node v comes from what refusing leaves: max(p_v - q_c, 0), or p_v without the refused tokens, by the inverse
-// of its running sum.  That is the work: one row (with q two) of the vocabulary per sequence is read, by `chunks` workgroups that
-// all do the walk for themselves; the workgroup that arrives last takes the sums of the pieces, and reads the piece that holds
-// the token once more.  All sums are held in 64 bits: the border between two tokens is to be found where the sum of 10^5 values
-// has it, and the tests take products of two 32-bit values, which 64 bits hold exactly.
+// of its running sum.  That is the work: one row (with q two) of the vocabulary per sequence is read.  A wave sums a piece of 4 KiB of it
+// at a time, all loads of a piece on their way together; the workgroups of a sequence all do the walk for themselves, and the one that
+// arrives last finds the token's piece by the sums and reads it once more.  All sums are held in 64 bits: the border between two tokens
+// is to be found where the sum of 10^5 values has it, and the tests take products of two 32-bit values, which 64 bits hold exactly.
 constexpr int kVerifyThreads = 256;
-constexpr int kVerifyChunkMax = 16384;
+constexpr int kVerifyWaves = kVerifyThreads / 64;
+constexpr int kPieceLoads = 4;                           // 16-byte loads of a lane for a piece
+constexpr int kMaxPieces = 4;                            // pieces of a wave
+constexpr int kMaxChunk = kMaxPieces * kVerifyWaves * kPieceLoads * 64 * 8;   // elements of a workgroup
 static_assert(kMaxVerifyNodes == kVerifyThreads, "a thread per node");
 
 template <class T>
@@ -249,16 +252,14 @@ struct RowVector<uint16_t> {
 };
 // N elements of a row from index i on; those past the row's end are 0.
 template <class T>
-OOCO_DEV void load_row(const T *row, int i, int size, float (&x)[RowVector<T>::N])
+OOCO_DEV void load_row(const T *row, int i, int size, typename RowVector<T>::type &v)
 {
     using R = RowVector<T>;
     if (i + R::N <= size) {
-        const typename R::type v = *reinterpret_cast<const typename R::type *>(row + i);
-#pragma unroll
-        for (int e = 0; e < R::N; ++e) x[e] = R::get(v, e);
+        v = *reinterpret_cast<const typename R::type *>(row + i);
     } else {
 #pragma unroll
-        for (int e = 0; e < R::N; ++e) x[e] = i + e < size ? R::value(row[i + e]) : 0.f;
+        for (int e = 0; e < R::N; ++e) v[e] = i + e < size ? row[i + e] : (T)0;
     }
 }
 OOCO_DEV double wave_sum(double v)
@@ -280,25 +281,25 @@ OOCO_DEV double wave_prefix(double v, int lane)   // inclusive
 template <class T, bool DRAFT>
 __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(const VerifyArgs a)
 {
-    constexpr int VEC = RowVector<T>::N;
-    constexpr int PASS = kVerifyThreads * VEC;
-    __shared__ int par[kMaxVerifyNodes], tok[kMaxVerifyNodes], first_child[kMaxVerifyNodes], walk[kMaxVerifyNodes];
-    __shared__ double prob[kMaxVerifyNodes];
-    __shared__ uint32_t refused[kVerifyChunkMax / 32];   // tokens of the piece that have been refused
-    __shared__ double wsum[kVerifyThreads / 64][2];
-    __shared__ int sh_len, sh_last, sh_found, sh_any, sh_chunk;
-    __shared__ double sh_base, sh_aim;
-    __shared__ int sh_use_full;
+    using R = RowVector<T>;
+    constexpr int VEC = R::N, PIECE = kPieceLoads * 64 * VEC;
+    __shared__ int4 par4[kMaxVerifyNodes / 4], tok4[kMaxVerifyNodes / 4];
+    __shared__ double2 prob2[kMaxVerifyNodes / 2];
+    __shared__ int first_child[kMaxVerifyNodes], walk[kMaxVerifyNodes];
+    __shared__ uint32_t refused[kMaxChunk / 32];   // tokens of the workgroup's elements that have been refused
+    __shared__ int sh_len, sh_last;
+    int *const par = reinterpret_cast<int *>(par4), *const tok = reinterpret_cast<int *>(tok4);
+    double *const prob = reinterpret_cast<double *>(prob2);
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int seq = blockIdx.x / a.chunks, piece = blockIdx.x - seq * a.chunks;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int seq = blockIdx.x / a.groups, group = blockIdx.x - seq * a.groups;
     int q0, n;
     rows_of(a.query_start_loc, seq, a.total_q, q0, n);
     n = min(n, kMaxVerifyNodes);
     int32_t *const path = a.path + (int64_t)seq * a.max_path;
     int32_t *const out = a.out_tokens + (int64_t)seq * (a.max_path + 1);
     if (n == 0) {
-        if (piece == 0) {
+        if (group == 0) {
             if (tid == 0) a.counts[seq] = 0;
             for (int i = tid; i <= a.max_path; i += kVerifyThreads) {
                 if (i < a.max_path) path[i] = -1;
@@ -317,29 +318,49 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(const VerifyArgs
         my_par = a.parents ? a.parents[q0 + tid] : tid - 1;
         if (my_par >= tid || my_par < 0) my_par = -1;
         my_tok = a.tokens[q0 + tid];
-        if (my_par >= 0) my_u = a.uniforms[q0 + tid];
+        my_u = a.uniforms[q0 + tid];
         if (my_par >= 0 && my_tok >= 0 && my_tok < a.vocab) {
-            my_p = RowVector<T>::value(target[my_par * a.stride + my_tok]);
-            if (DRAFT) my_q = RowVector<T>::value(draft[tid * a.stride + my_tok]);
+            my_p = R::value(target[my_par * a.stride + my_tok]);
+            if (DRAFT) my_q = R::value(draft[tid * a.stride + my_tok]);
         }
     }
     par[tid] = my_par;
     tok[tid] = my_tok;
     first_child[tid] = INT_MAX;
+    const int chunk = a.pieces * kVerifyWaves * PIECE;     // elements of the workgroup
+    const int64_t c0 = (int64_t)group * chunk;
+    if (!DRAFT)
+        for (int i = tid; i < chunk / 32; i += kVerifyThreads) refused[i] = 0;
     __syncthreads();
     double rest = 1.0;
     if (a.parents) {
-        if (my_par >= 0)
-            for (int j = 1; j < tid; ++j)   // (a token that a sibling has had already is not there any more)
-                if (par[j] == my_par && tok[j] == my_tok) my_p = 0.0;
+        // (nodes of the wave look at all nodes before its last one, four at a time)
+        const int looks = (min(n, 64 * wave + 64) + 3) / 4;
+        if (my_par >= 0) {
+            bool again = false;   // a token that a sibling has had already is not there any more
+#pragma unroll 4
+            for (int j = 0; j < looks; ++j) {
+                const int4 pj = par4[j], tj = tok4[j];
+                again |= (pj.x == my_par && tj.x == my_tok && 4 * j < tid) || (pj.y == my_par && tj.y == my_tok && 4 * j + 1 < tid) ||
+                         (pj.z == my_par && tj.z == my_tok && 4 * j + 2 < tid) || (pj.w == my_par && tj.w == my_tok && 4 * j + 3 < tid);
+            }
+            if (again) my_p = 0.0;
+        }
         prob[tid] = my_p;
         __syncthreads();
-        if (my_par >= 0)
-            for (int j = 1; j < tid; ++j)
-                if (par[j] == my_par) rest -= prob[j];
+        if (my_par >= 0) {
+#pragma unroll 4
+            for (int j = 0; j < looks; ++j) {
+                const int4 pj = par4[j];
+                const double2 u = prob2[2 * j], v = prob2[2 * j + 1];
+                rest -= pj.x == my_par && 4 * j < tid ? u.x : 0.0;
+                rest -= pj.y == my_par && 4 * j + 1 < tid ? u.y : 0.0;
+                rest -= pj.z == my_par && 4 * j + 2 < tid ? v.x : 0.0;
+                rest -= pj.w == my_par && 4 * j + 3 < tid ? v.y : 0.0;
+            }
+        }
     }
     if (my_par >= 0 && my_u * my_q * rest < my_p) atomicMin(&first_child[my_par], tid);
-    for (int i = tid; i < a.chunk / 32; i += kVerifyThreads) refused[i] = 0;
     __syncthreads();
     if (tid == 0) {
         int at = 0, len = 0;
@@ -351,180 +372,179 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(const VerifyArgs
         }
         sh_len = len;
         sh_last = at;
-        sh_found = INT_MAX;
-        sh_any = -1;
     }
     __syncthreads();
     const int len = sh_len, last = sh_last;
     // (a path that ends for want of room refuses nobody)
     const bool refuses = len < a.max_path;
-    const int c0 = piece * a.chunk;
-    if (!DRAFT && refuses && my_par == last && my_tok >= c0 && my_tok - c0 < a.chunk && my_tok < a.vocab)
-        atomicOr(&refused[(my_tok - c0) / 32], 1u << ((my_tok - c0) & 31));
+    auto mark = [&](int64_t first) {
+        if (!DRAFT && refuses && my_par == last && my_tok >= first && my_tok < first + chunk && my_tok < a.vocab)
+            atomicOr(&refused[(my_tok - first) / 32], 1u << ((my_tok - first) & 31));
+    };
+    mark(c0);
     __syncthreads();
     const T *const p_row = target + last * a.stride;
     const bool minus = DRAFT && refuses && last + 1 < n;
     const T *const q_row = draft + (minus ? last + 1 : 0) * a.stride;
 
-    // weights of elements i .. i + VEC of the row: what is left (w) and what there was (f); b: bit of element i in `refused`
-    auto weights = [&](int i, int b, float (&f)[VEC], double (&w)[VEC]) {
-        float q[VEC];
-        load_row(p_row, i, a.vocab, f);
-        if (minus) load_row(q_row, i, a.vocab, q);
+    // The piece from element i0 on, of which the lane has elements i0 + 64 VEC j + VEC lane + e: what there was, and what is left.
+    typename R::type pv[kPieceLoads], qv[kPieceLoads];
+    auto load_piece = [&](int i0) {
+#pragma unroll
+        for (int j = 0; j < kPieceLoads; ++j) load_row(p_row, i0 + (64 * j + lane) * VEC, a.vocab, pv[j]);
+        if (minus) {
+#pragma unroll
+            for (int j = 0; j < kPieceLoads; ++j) load_row(q_row, i0 + (64 * j + lane) * VEC, a.vocab, qv[j]);
+        }
+    };
+    auto weights = [&](int j, int64_t bit0, float (&f)[VEC], double (&w)[VEC]) {   // of load j; bit0: place of the piece in `refused`
+        const int b = (int)bit0 + (64 * j + lane) * VEC;
         const uint32_t bits = DRAFT ? 0u : refused[b / 32] >> (b & 31);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
+            f[e] = R::get(pv[j], e);
             f[e] = f[e] > 0.f && f[e] <= FLT_MAX ? f[e] : 0.f;
             double d = f[e];
-            if (minus) d -= (double)q[e];
+            if (minus) d -= (double)R::get(qv[j], e);
             w[e] = d > 0.0 && !((bits >> e) & 1u) ? d : 0.0;
         }
     };
-    const int c1 = (int)min((int64_t)a.vocab, (int64_t)c0 + a.chunk);
-    double left = 0.0, full = 0.0;
-    for (int i = c0 + tid * VEC; i < c1; i += PASS) {
-        float f[VEC];
-        double w[VEC];
-        weights(i, i - c0, f, w);
+    double *const sums = a.sums + (int64_t)seq * a.groups * (a.pieces * kVerifyWaves) * 2;
+    for (int k = 0; k < a.pieces; ++k) {
+        const int piece = (group * a.pieces + k) * kVerifyWaves + wave;   // of the row
+        const int64_t i0 = (int64_t)piece * PIECE;
+        double left = 0.0, full = 0.0;
+        if (i0 < a.vocab) {
+            load_piece((int)i0);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            left += w[e];
-            full += (double)f[e];
+            for (int j = 0; j < kPieceLoads; ++j) {
+                float f[VEC];
+                double w[VEC];
+                weights(j, i0 - c0, f, w);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    left += w[e];
+                    full += (double)f[e];
+                }
+            }
+            left = wave_sum(left);
+            full = wave_sum(full);
+        }
+        if (lane == 0) {
+            __hip_atomic_store(sums + 2 * piece, left, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __hip_atomic_store(sums + 2 * piece + 1, full, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
     }
-    left = wave_sum(left);
-    full = wave_sum(full);
-    if (lane == 0) {
-        wsum[wave][0] = left;
-        wsum[wave][1] = full;
-    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the sums have reached memory before the count
     __syncthreads();
-    double *const sums = a.sums + (int64_t)seq * a.chunks * 2;
     if (tid == 0) {
-        left = (wsum[0][0] + wsum[1][0]) + (wsum[2][0] + wsum[3][0]);
-        full = (wsum[0][1] + wsum[1][1]) + (wsum[2][1] + wsum[3][1]);
-        __hip_atomic_store(sums + 2 * piece, left, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        __hip_atomic_store(sums + 2 * piece + 1, full, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the sums have reached memory before the count
         const int prev = __hip_atomic_fetch_add(a.arrivals + seq, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        sh_last = prev == a.chunks - 1;
+        sh_last = prev == a.groups - 1;
     }
     __syncthreads();
     if (!sh_last) return;
 
-    // ---- the workgroup that arrived last: the piece, then the element
-    if (wave == 0) {
-        auto sum_at = [&](int i, int which) -> double {
-            return i < a.chunks ? __hip_atomic_load(sums + 2 * i + which, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
-        };
-        double total[2] = {0.0, 0.0};
-        for (int i = lane; i < a.chunks; i += 64) {
-            total[0] += sum_at(i, 0);
-            total[1] += sum_at(i, 1);
-        }
-        total[0] = wave_sum(total[0]);
-        total[1] = wave_sum(total[1]);
-        const int which = total[0] > 0.0 ? 0 : 1;   // (nothing left: the draw is from all there was)
-        const double aim = (double)a.final_uniforms[seq] * total[which];
-        double before = 0.0, base = 0.0;
-        int chunk = -1;                               // the first piece whose running sum passes the aim, or the last with a weight
-        for (int i0 = 0; i0 < a.chunks; i0 += 64) {
-            const double v = sum_at(i0 + lane, which);
-            const double run = before + wave_prefix(v, lane);
-            const uint64_t some = __ballot(v > 0.0), past = __ballot(v > 0.0 && run > aim);
-            const int k = past ? __ffsll((unsigned long long)past) - 1 : some ? 63 - __clzll((long long)some) : -1;
-            if (k >= 0) {
-                chunk = i0 + k;
-                base = __shfl(run - v, k);
-            }
-            if (past) break;
-            before = __shfl(run, 63);
-        }
-        if (lane == 0) {
-            sh_chunk = chunk;
-            sh_base = base;
-            sh_aim = aim;
-            sh_use_full = which;
-            __hip_atomic_store(a.arrivals + seq, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // ready for the next call
-        }
+    // ---- the workgroup that arrived last
+    if (tid == 0) {
+        a.counts[seq] = len + 1;
+        __hip_atomic_store(a.arrivals + seq, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // ready for the next call
     }
-    __syncthreads();
-    const int chunk = sh_chunk;
-    const double aim = sh_aim;
-    const bool use_full = sh_use_full;
-    if (chunk >= 0) {
-        const int b0 = chunk * a.chunk;
-        if (!DRAFT && chunk != piece) {
-            for (int i = tid; i < a.chunk / 32; i += kVerifyThreads) refused[i] = 0;
+    for (int i = tid; i <= a.max_path; i += kVerifyThreads) {
+        if (i < a.max_path) path[i] = i < len ? walk[i] : -1;
+        if (i != len) out[i] = i < len ? tok[walk[i]] : -1;
+    }
+    const int pieces = a.groups * a.pieces * kVerifyWaves;
+    auto sum_at = [&](int i, int which) -> double {
+        return i < pieces ? __hip_atomic_load(sums + 2 * i + which, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
+    };
+    // Every wave finds the piece (all the same): the first whose running sum passes the aim, or the last with a weight.
+    double total[2] = {0.0, 0.0};
+    for (int i = lane; i < pieces; i += 64) {
+        total[0] += sum_at(i, 0);
+        total[1] += sum_at(i, 1);
+    }
+    total[0] = wave_sum(total[0]);
+    total[1] = wave_sum(total[1]);
+    const bool use_full = !(total[0] > 0.0);        // (nothing left: the draw is from all there was)
+    const double aim = (double)a.final_uniforms[seq] * total[use_full];
+    double before = 0.0, base = 0.0;
+    int found_piece = -1;
+    for (int i0 = 0; i0 < pieces; i0 += 64) {
+        const double v = sum_at(i0 + lane, use_full);
+        const double run = before + wave_prefix(v, lane);
+        const uint64_t some = __ballot(v > 0.0), past = __ballot(v > 0.0 && run > aim);
+        const int k = past ? __ffsll((unsigned long long)past) - 1 : some ? 63 - __clzll((long long)some) : -1;
+        if (k >= 0) {
+            found_piece = i0 + k;
+            base = __shfl(run - v, k);
+        }
+        if (past) break;
+        before = __shfl(run, 63);
+    }
+    int drawn = -1;
+    if (found_piece >= 0) {
+        const int i0 = found_piece * PIECE;
+        const int64_t first = (int64_t)(found_piece / (a.pieces * kVerifyWaves)) * chunk;   // of the workgroup whose piece it is
+        if (!DRAFT && first != c0) {
             __syncthreads();
-            if (refuses && my_par == last && my_tok >= b0 && my_tok - b0 < a.chunk && my_tok < a.vocab)
-                atomicOr(&refused[(my_tok - b0) / 32], 1u << ((my_tok - b0) & 31));
+            for (int i = tid; i < chunk / 32; i += kVerifyThreads) refused[i] = 0;
+            __syncthreads();
+            mark(first);
             __syncthreads();
         }
-        const int b1 = (int)min((int64_t)a.vocab, (int64_t)b0 + a.chunk);
-        double base = sh_base;
-        for (int i0 = b0; i0 < b1; i0 += PASS) {   // (the same passes for every thread)
-            const int i = i0 + tid * VEC;
-            float f[VEC];
-            double w[VEC];
+        if (wave != 0) return;
+        load_piece(i0);
+        int found = INT_MAX, any = -1;
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                f[e] = 0.f;
-                w[e] = 0.0;
-            }
-            if (i < b1) weights(i, i - b0, f, w);
-            double own = 0.0;
+        for (int j = 0; j < kPieceLoads; ++j) {
+            float f[VEC];
+            double w[VEC], own = 0.0;
+            weights(j, i0 - first, f, w);
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 if (use_full) w[e] = f[e];
                 own += w[e];
             }
             const double incl = wave_prefix(own, lane);
-            if (lane == 63) wsum[wave][0] = incl;
-            __syncthreads();
             double run = base + incl - own;
-            for (int k = 0; k < wave; ++k) run += wsum[k][0];
-            int found = INT_MAX, any = -1;
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 run += w[e];
                 if (w[e] > 0.0) {
-                    any = i + e;
-                    if (run > aim && found == INT_MAX) found = i + e;
+                    const int i = i0 + (64 * j + lane) * VEC + e;
+                    any = i;
+                    if (run > aim && found == INT_MAX) found = i;
                 }
             }
-            if (found != INT_MAX) atomicMin(&sh_found, found);
-            if (any >= 0) atomicMax(&sh_any, any);
-            base += (wsum[0][0] + wsum[1][0]) + (wsum[2][0] + wsum[3][0]);
-            __syncthreads();
-            if (sh_found != INT_MAX) break;
+            base += __shfl(incl, 63);
         }
+#pragma unroll
+        for (int d = 32; d; d >>= 1) {
+            found = min(found, __shfl_xor(found, d));
+            any = max(any, __shfl_xor(any, d));
+        }
+        drawn = found != INT_MAX ? found : any;
     }
-    __syncthreads();
-    const int drawn = sh_found != INT_MAX ? sh_found : sh_any;
-    if (tid == 0) a.counts[seq] = len + 1;
-    for (int i = tid; i <= a.max_path; i += kVerifyThreads) {
-        if (i < a.max_path) path[i] = i < len ? walk[i] : -1;
-        out[i] = i < len ? tok[walk[i]] : i == len ? drawn : -1;
-    }
+    if (tid == 0) out[len] = drawn;
 }
 
-void verify_chunks(VerifyArgs &a, int num_cus)
+void verify_layout(VerifyArgs &a, bool bf16, int num_cus)
 {
-    // pieces that give every compute unit four workgroups, of 2048 to 16,384 elements
-    constexpr int64_t unit = 2048;
-    const int64_t want = (int64_t)a.vocab * a.num_seqs / (4 * num_cus);
-    a.chunk = (int)std::min<int64_t>(kVerifyChunkMax, std::max<int64_t>(1, (want + unit - 1) / unit) * unit);
-    a.chunks = (a.vocab + a.chunk - 1) / a.chunk;
+    // As many pieces for a wave, 1, 2 or 4, as leave eight workgroups to a compute unit.
+    const int piece = kPieceLoads * 64 * (bf16 ? 8 : 4);
+    const int64_t pieces = ((int64_t)a.vocab + piece - 1) / piece;
+    a.pieces = 1;
+    while (a.pieces < kMaxPieces && pieces * a.num_seqs > (int64_t)8 * num_cus * kVerifyWaves * a.pieces) a.pieces *= 2;
+    a.groups = (int)((pieces + kVerifyWaves * a.pieces - 1) / (kVerifyWaves * a.pieces));
 }
 
-size_t verify_workspace(const VerifyArgs &a) { return (size_t)a.num_seqs * (size_t)a.chunks * 2 * sizeof(double); }
+size_t verify_workspace(const VerifyArgs &a) { return (size_t)a.num_seqs * (size_t)a.groups * (a.pieces * kVerifyWaves) * 2 * sizeof(double); }
 
 hipError_t launch_verify(const VerifyArgs &a, bool bf16, hipStream_t s)
 {
     auto *const kernel = bf16 ? (a.draft ? verify_kernel<uint16_t, true> : verify_kernel<uint16_t, false>)
                               : (a.draft ? verify_kernel<float, true> : verify_kernel<float, false>);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)a.num_seqs * a.chunks)), dim3(kVerifyThreads), 0, s, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)a.num_seqs * a.groups)), dim3(kVerifyThreads), 0, s, a);
     return hipGetLastError();
 }
 

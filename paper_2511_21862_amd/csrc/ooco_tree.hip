@@ -770,7 +770,16 @@ hipError_t launch(TreeArgs &a, void *ws, hipStream_t s)
 }
 }  // namespace
 
-int tree_waves(int total_q, int num_seqs, int g) { return (int64_t)total_q * g > 128 * (int64_t)num_seqs ? 8 : 4; }
+// Workgroups of eight waves fetch K and V once for 256 columns where four waves fetch them twice, at about the same time if the lengths
+// are equal and at different times if not; they are fewer, and their waves wait for one another.  So they are for sequences of more
+// than 128 columns on average, and for work that fills them: 16 steps each, of what the block tables can hold (the lengths are on the
+// device).  MI355X, us, four / eight waves, 64 nodes of 32/8 heads: 4 sequences of 1000 tokens 33 / 37, 4 of 4000 43 / 47, 32 of 4096 168 /
+// 163, 64 of 4096 411 / 321; 4 x 20..27 nodes of 28/4 heads on 60..131K 308 / 226.
+int tree_waves(int total_q, int num_seqs, int Hkv, int g, int max_blocks_per_seq, int num_cus)
+{
+    const double steps = (double)num_seqs * Hkv * ((double)max_blocks_per_seq * kBlockSize / kTreeStep);
+    return (int64_t)total_q * g > 128 * (int64_t)num_seqs && steps >= 16.0 * num_cus ? 8 : 4;
+}
 
 int tree_runs_log2(int waves, int hd, int num_cus, size_t ws_bytes)
 {

@@ -298,6 +298,19 @@ def test_attn_tree_long_contexts_are_cut_and_merged(heads):
         check_attn(b, masks, workspace_bytes=600 << 10)                              # a workspace of two runs
 
 
+@pytest.mark.parametrize("heads", [HEADS[0], HEADS[2], HEADS[3]], ids=str)
+def test_attn_tree_of_wide_trees_and_large_tables(heads):
+    # more than 128 columns a sequence and block tables of a capacity that calls for workgroups of eight waves: tiles of every width
+    for nodes, ctx, words in (([64, 50, 64], [300, 1000, 17], 1), ([200, 130, 3, 0, 1, 70], [100, 0, 700, 5, 31, 64], 4), ([64], [9000], 1)):
+        Hq, Hkv, hd = heads
+        b = batch(heads, nodes, ctx, seed=435, poison=len(nodes) > 1, max_blocks_per_seq=-(-16 * 256 * 8 // (len(nodes) * Hkv)) + 1)
+        masks, _ = S.tree_masks(trees(nodes, np.random.default_rng(3)), b.query_start_loc, b.ctx_lens, words)
+        say(f"case: tree attention of wide trees {heads} nodes={nodes}")
+        first = run_attn(b, masks)
+        check_attn(b, masks, first)
+        assert (run_attn(b, masks) == first).all()
+
+
 def test_attn_tree_many_sequences():
     # more sequences than a workgroup looks at in one go
     rng = np.random.default_rng(4)
