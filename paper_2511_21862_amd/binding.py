@@ -115,7 +115,9 @@ if torch is not None:
         if getattr(_native, "BUILT_FOR", None) != _built_for(torch):
             raise ImportError(f"built as '{getattr(_native, 'BUILT_FOR', None)}'")
         _native.bind(_P, *[ctypes.cast(f, _P).value for f in (_lib.ooco_plan, _lib.ooco_attn_mixed, _lib.ooco_attn_mixed_static,
-                                                              _lib.ooco_kv_append, _lib.ooco_kv_block_copy)])
+                                                              _lib.ooco_kv_append, _lib.ooco_kv_block_copy, _lib.ooco_tree_masks,
+                                                              _lib.ooco_rope_append, _lib.ooco_attn_tree, _lib.ooco_verify_drafts,
+                                                              _lib.ooco_kv_compact)])
     except ImportError as e:      # not built, or built for another torch: the general way alone
         import warnings
 
@@ -131,6 +133,9 @@ def _not_native(*args):
 _OF_TENSOR = getattr(_native, "OF_TENSOR", None)     # for a size: the native module reads it off the tensor
 _plan_fast, _attn_fast, _static_fast, _append_fast, _copy_fast = (
     (_native.plan, _native.attn_mixed, _native.attn_mixed_static, _native.kv_append, _native.kv_block_copy)
+    if _native is not None else (_not_native,) * 5)
+_masks_fast, _rope_fast, _tree_fast, _verify_fast, _compact_fast = (
+    (_native.tree_masks, _native.rope_append, _native.attn_tree, _native.verify_drafts, _native.kv_compact)
     if _native is not None else (_not_native,) * 5)
 
 
@@ -335,6 +340,9 @@ def ooco_kv_append(ctx, k_new, v_new, k_cache, v_cache, block_tables, query_star
 
 
 def ooco_tree_masks(ctx, parents, query_start_loc, ctx_lens, masks, positions, mask_words, num_seqs, total_q_tokens, stream=None) -> None:
+    st = _masks_fast(ctx, parents, query_start_loc, ctx_lens, masks, positions, mask_words, num_seqs, total_q_tokens, stream)
+    if st is not NotImplemented:
+        return _check(ctx, st)
     _check(ctx, _lib.ooco_tree_masks(ctx, _dev(parents), _dev(query_start_loc), _dev(ctx_lens), _dev(masks), _dev(positions), mask_words,
                                      num_seqs, total_q_tokens, _stream_handle(stream)))
 
@@ -378,6 +386,10 @@ def _rows(t):
 def ooco_rope_append(ctx, q, k_new, v_new, positions, q_out, k_cache, v_cache, block_tables, query_start_loc, ctx_lens, num_seqs,
                      total_q_tokens, stream=None) -> None:
     """q, k_new and v_new may be views of a wider tensor (rows contiguous, any distance between them)."""
+    st = _rope_fast(ctx, q, k_new, v_new, positions, q_out, k_cache, v_cache, block_tables, query_start_loc, ctx_lens, num_seqs, total_q_tokens,
+                    stream)
+    if st is not NotImplemented:
+        return _check(ctx, st)
     _check(ctx, _lib.ooco_rope_append(ctx, *_rows(q), *_rows(k_new), *_rows(v_new), _dev(positions), _dev(q_out), _dev(k_cache),
                                       _dev(v_cache), _dev(block_tables), _dev(query_start_loc), _dev(ctx_lens), num_seqs,
                                       total_q_tokens, _stream_handle(stream)))
@@ -385,6 +397,9 @@ def ooco_rope_append(ctx, q, k_new, v_new, positions, q_out, k_cache, v_cache, b
 
 def ooco_attn_tree(ctx, q, k_cache, v_cache, block_tables, query_start_loc, ctx_lens, masks, mask_words, out, num_seqs, total_q_tokens,
                    stream=None) -> None:
+    st = _tree_fast(ctx, q, k_cache, v_cache, block_tables, query_start_loc, ctx_lens, masks, mask_words, out, num_seqs, total_q_tokens, stream)
+    if st is not NotImplemented:
+        return _check(ctx, st)
     _check(ctx, _lib.ooco_attn_tree(ctx, _dev(q), _dev(k_cache), _dev(v_cache), _dev(block_tables), _dev(query_start_loc),
                                     _dev(ctx_lens), _dev(masks), mask_words, _dev(out), num_seqs, total_q_tokens,
                                     _stream_handle(stream)))
@@ -393,6 +408,10 @@ def ooco_attn_tree(ctx, q, k_cache, v_cache, block_tables, query_start_loc, ctx_
 def ooco_verify_drafts(ctx, target_probs, draft_probs, tokens, parents, uniforms, final_uniforms, query_start_loc, counts, path,
                        out_tokens, max_path, num_seqs, total_q_tokens, stream=None) -> None:
     """target_probs, draft_probs: float32 or bfloat16 [rows][vocab], rows contiguous, equally far apart in both."""
+    st = _verify_fast(ctx, target_probs, draft_probs, tokens, parents, uniforms, final_uniforms, query_start_loc, counts, path, out_tokens,
+                      max_path, num_seqs, total_q_tokens, stream)
+    if st is not NotImplemented:
+        return _check(ctx, st)
     if target_probs.dtype not in (torch.float32, torch.bfloat16) or (draft_probs is not None and draft_probs.dtype != target_probs.dtype):
         raise ValueError("probabilities are float32 or bfloat16, the draft's as the target's")
     if target_probs.stride(1) != 1 or (draft_probs is not None and draft_probs.stride() != target_probs.stride()):
@@ -406,6 +425,9 @@ def ooco_verify_drafts(ctx, target_probs, draft_probs, tokens, parents, uniforms
 
 def ooco_kv_compact(ctx, k_caches, v_caches, block_tables, ctx_lens, path, counts, max_path, num_seqs, stream=None) -> None:
     """k_caches, v_caches: the pools of all layers, one tensor each."""
+    st = _compact_fast(ctx, k_caches, v_caches, block_tables, ctx_lens, path, counts, max_path, num_seqs, stream)
+    if st is not NotImplemented:
+        return _check(ctx, st)
     n = len(k_caches)
     if len(v_caches) != n:
         raise ValueError(f"{n} pools of K and {len(v_caches)} of V")
@@ -582,6 +604,9 @@ class Context:
         ooco_kv_block_copy(self.h, k_src, v_src, k_dst, v_dst, src_ids, dst_ids, int(src_ids.shape[0]), stream)
 
     def tree_masks(self, parents, query_start_loc, ctx_lens, masks, positions=None, stream=None):
+        st = _masks_fast(self.h, parents, query_start_loc, ctx_lens, masks, positions, _OF_TENSOR, _OF_TENSOR, _OF_TENSOR, stream)
+        if st is not NotImplemented:
+            return _check(self.h, st)
         ooco_tree_masks(self.h, parents, query_start_loc, ctx_lens, masks, positions, int(masks.shape[1]), int(ctx_lens.shape[0]),
                         int(parents.shape[0]), stream)
 
@@ -589,18 +614,32 @@ class Context:
         ooco_rope_set(self.h, 2 * len(frequencies), interleaved, frequencies, factor)
 
     def rope_append(self, q, k_new, v_new, q_out, k_cache, v_cache, block_tables, query_start_loc, ctx_lens, positions=None, stream=None):
+        st = _rope_fast(self.h, q, k_new, v_new, positions, q_out, k_cache, v_cache, block_tables, query_start_loc, ctx_lens, _OF_TENSOR,
+                        _OF_TENSOR, stream)
+        if st is not NotImplemented:
+            return _check(self.h, st)
         ooco_rope_append(self.h, q, k_new, v_new, positions, q_out, k_cache, v_cache, block_tables, query_start_loc, ctx_lens,
                          int(ctx_lens.shape[0]), int(q.shape[0]), stream)
 
     def attn_tree(self, q, k_cache, v_cache, block_tables, query_start_loc, ctx_lens, masks, out, stream=None):
+        st = _tree_fast(self.h, q, k_cache, v_cache, block_tables, query_start_loc, ctx_lens, masks, _OF_TENSOR, out, _OF_TENSOR, _OF_TENSOR, stream)
+        if st is not NotImplemented:
+            return _check(self.h, st)
         ooco_attn_tree(self.h, q, k_cache, v_cache, block_tables, query_start_loc, ctx_lens, masks, int(masks.shape[1]), out,
                        int(ctx_lens.shape[0]), int(q.shape[0]), stream)
 
     def verify_drafts(self, target_probs, tokens, uniforms, final_uniforms, query_start_loc, counts, path, out_tokens, draft_probs=None,
                       parents=None, stream=None):
+        st = _verify_fast(self.h, target_probs, draft_probs, tokens, parents, uniforms, final_uniforms, query_start_loc, counts, path, out_tokens,
+                          _OF_TENSOR, _OF_TENSOR, _OF_TENSOR, stream)
+        if st is not NotImplemented:
+            return _check(self.h, st)
         ooco_verify_drafts(self.h, target_probs, draft_probs, tokens, parents, uniforms, final_uniforms, query_start_loc, counts, path,
                            out_tokens, int(path.shape[1]), int(counts.shape[0]), int(tokens.shape[0]), stream)
 
     def kv_compact(self, k_caches, v_caches, block_tables, ctx_lens, path, counts, stream=None):
+        st = _compact_fast(self.h, k_caches, v_caches, block_tables, ctx_lens, path, counts, _OF_TENSOR, _OF_TENSOR, stream)
+        if st is not NotImplemented:
+            return _check(self.h, st)
         ooco_kv_compact(self.h, k_caches, v_caches, block_tables, ctx_lens, path, counts, int(path.shape[1]), int(ctx_lens.shape[0]),
                         stream)

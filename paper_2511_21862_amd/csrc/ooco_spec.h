@@ -73,7 +73,8 @@ struct VerifyArgs {
     const int32_t *query_start_loc;
     int32_t *counts, *path, *out_tokens;
     double *sums;                        // [num_seqs][pieces of a row][2]: what is left, and what there was
-    int32_t *arrivals;                   // [num_seqs], zero between calls
+    int32_t *arrivals;                   // of each sequence, arrivals_apart ints apart, zero between calls
+    int32_t arrivals_apart;
     int64_t stride;
     int32_t vocab, max_path;
     int32_t num_seqs, total_q;

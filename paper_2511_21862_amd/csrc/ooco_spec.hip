@@ -262,34 +262,44 @@ OOCO_DEV void load_row(const T *row, int i, int size, typename RowVector<T>::typ
         for (int e = 0; e < R::N; ++e) v[e] = i + e < size ? row[i + e] : (T)0;
     }
 }
-OOCO_DEV double wave_sum(double v)
+// Inclusive sum over the lanes of a wave, and the sum of all: four shifts within rows of 16 lanes, then the last lane of a row to the
+// rows behind it, twice -- moves of the vector ALU, where a shuffle through LDS takes a hundred cycles a stage.
+template <int CTRL, int ROWS>
+OOCO_DEV double moved(double v)   // 0 in lanes that nothing is moved to
 {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, ROWS, 0xF, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(u >> 32), CTRL, ROWS, 0xF, false);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+OOCO_DEV double wave_prefix(double v)
+{
+    v += moved<0x111, 0xF>(v);   // row_shr 1, 2, 4, 8
+    v += moved<0x112, 0xF>(v);
+    v += moved<0x114, 0xF>(v);
+    v += moved<0x118, 0xF>(v);
+    v += moved<0x142, 0xA>(v);   // row_bcast 15 to rows 1 and 3, 31 to rows 2 and 3
+    v += moved<0x143, 0xC>(v);
     return v;
 }
-OOCO_DEV double wave_prefix(double v, int lane)   // inclusive
+OOCO_DEV double lane_of(double v, int lane)   // wave-uniform lane
 {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const double o = __shfl_up(v, d);
-        v += lane >= d ? o : 0.0;
-    }
-    return v;
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)u, lane), hi = __builtin_amdgcn_readlane((int)(u >> 32), lane);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
+OOCO_DEV double wave_sum(double v) { return lane_of(wave_prefix(v), 63); }
 
 template <class T, bool DRAFT>
 __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(const VerifyArgs a)
 {
     using R = RowVector<T>;
     constexpr int VEC = R::N, PIECE = kPieceLoads * 64 * VEC;
-    __shared__ int4 par4[kMaxVerifyNodes / 4], tok4[kMaxVerifyNodes / 4];
-    __shared__ double2 prob2[kMaxVerifyNodes / 2];
-    __shared__ int first_child[kMaxVerifyNodes], walk[kMaxVerifyNodes];
+    __shared__ double prob[kMaxVerifyNodes];
+    __shared__ int tok[kMaxVerifyNodes], sibling[kMaxVerifyNodes], first_child[kMaxVerifyNodes], walk[kMaxVerifyNodes];
+    __shared__ uint32_t children[DRAFT ? 1 : kMaxVerifyNodes][kMaxVerifyNodes / 32];
     __shared__ uint32_t refused[kMaxChunk / 32];   // tokens of the workgroup's elements that have been refused
     __shared__ int sh_len, sh_last;
-    int *const par = reinterpret_cast<int *>(par4), *const tok = reinterpret_cast<int *>(tok4);
-    double *const prob = reinterpret_cast<double *>(prob2);
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int seq = blockIdx.x / a.groups, group = blockIdx.x - seq * a.groups;
@@ -324,41 +334,36 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(const VerifyArgs
             if (DRAFT) my_q = R::value(draft[tid * a.stride + my_tok]);
         }
     }
-    par[tid] = my_par;
     tok[tid] = my_tok;
     first_child[tid] = INT_MAX;
+    if (!DRAFT && a.parents) {
+#pragma unroll
+        for (int w = 0; w < kMaxVerifyNodes / 32; ++w) children[tid][w] = 0;
+    }
     const int chunk = a.pieces * kVerifyWaves * PIECE;     // elements of the workgroup
     const int64_t c0 = (int64_t)group * chunk;
     if (!DRAFT)
         for (int i = tid; i < chunk / 32; i += kVerifyThreads) refused[i] = 0;
     __syncthreads();
     double rest = 1.0;
-    if (a.parents) {
-        // (nodes of the wave look at all nodes before its last one, four at a time)
-        const int looks = (min(n, 64 * wave + 64) + 3) / 4;
-        if (my_par >= 0) {
-            bool again = false;   // a token that a sibling has had already is not there any more
-#pragma unroll 4
-            for (int j = 0; j < looks; ++j) {
-                const int4 pj = par4[j], tj = tok4[j];
-                again |= (pj.x == my_par && tj.x == my_tok && 4 * j < tid) || (pj.y == my_par && tj.y == my_tok && 4 * j + 1 < tid) ||
-                         (pj.z == my_par && tj.z == my_tok && 4 * j + 2 < tid) || (pj.w == my_par && tj.w == my_tok && 4 * j + 3 < tid);
-            }
-            if (again) my_p = 0.0;
-        }
-        prob[tid] = my_p;
+    if (!DRAFT && a.parents) {
+        // The sibling before each node, by the children of each node as bits.
+        int older = -1;
+        if (my_par >= 0) atomicOr(&children[my_par][tid / 32], 1u << (tid & 31));
         __syncthreads();
         if (my_par >= 0) {
-#pragma unroll 4
-            for (int j = 0; j < looks; ++j) {
-                const int4 pj = par4[j];
-                const double2 u = prob2[2 * j], v = prob2[2 * j + 1];
-                rest -= pj.x == my_par && 4 * j < tid ? u.x : 0.0;
-                rest -= pj.y == my_par && 4 * j + 1 < tid ? u.y : 0.0;
-                rest -= pj.z == my_par && 4 * j + 2 < tid ? v.x : 0.0;
-                rest -= pj.w == my_par && 4 * j + 3 < tid ? v.y : 0.0;
-            }
+            int w = tid / 32;
+            uint32_t before = children[my_par][w] & ((1u << (tid & 31)) - 1u);
+            while (!before && w > 0) before = children[my_par][--w];
+            if (before) older = 32 * w + 31 - __clz((int)before);
         }
+        sibling[tid] = older;
+        __syncthreads();
+        for (int j = older; j >= 0; j = sibling[j])   // a token that a sibling has had already is not there any more
+            if (tok[j] == my_tok) my_p = 0.0;
+        prob[tid] = my_p;
+        __syncthreads();
+        for (int j = older; j >= 0; j = sibling[j]) rest -= prob[j];
     }
     if (my_par >= 0 && my_u * my_q * rest < my_p) atomicMin(&first_child[my_par], tid);
     __syncthreads();
@@ -438,7 +443,7 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(const VerifyArgs
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the sums have reached memory before the count
     __syncthreads();
     if (tid == 0) {
-        const int prev = __hip_atomic_fetch_add(a.arrivals + seq, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const int prev = __hip_atomic_fetch_add(a.arrivals + (int64_t)seq * a.arrivals_apart, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         sh_last = prev == a.groups - 1;
     }
     __syncthreads();
@@ -447,7 +452,7 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(const VerifyArgs
     // ---- the workgroup that arrived last
     if (tid == 0) {
         a.counts[seq] = len + 1;
-        __hip_atomic_store(a.arrivals + seq, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // ready for the next call
+        __hip_atomic_store(a.arrivals + (int64_t)seq * a.arrivals_apart, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // ready for the next call
     }
     for (int i = tid; i <= a.max_path; i += kVerifyThreads) {
         if (i < a.max_path) path[i] = i < len ? walk[i] : -1;
@@ -471,15 +476,15 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(const VerifyArgs
     int found_piece = -1;
     for (int i0 = 0; i0 < pieces; i0 += 64) {
         const double v = sum_at(i0 + lane, use_full);
-        const double run = before + wave_prefix(v, lane);
+        const double run = before + wave_prefix(v);
         const uint64_t some = __ballot(v > 0.0), past = __ballot(v > 0.0 && run > aim);
         const int k = past ? __ffsll((unsigned long long)past) - 1 : some ? 63 - __clzll((long long)some) : -1;
         if (k >= 0) {
             found_piece = i0 + k;
-            base = __shfl(run - v, k);
+            base = lane_of(run - v, k);
         }
         if (past) break;
-        before = __shfl(run, 63);
+        before = lane_of(run, 63);
     }
     int drawn = -1;
     if (found_piece >= 0) {
@@ -505,18 +510,16 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(const VerifyArgs
                 if (use_full) w[e] = f[e];
                 own += w[e];
             }
-            const double incl = wave_prefix(own, lane);
+            const double incl = wave_prefix(own);
             double run = base + incl - own;
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 run += w[e];
-                if (w[e] > 0.0) {
-                    const int i = i0 + (64 * j + lane) * VEC + e;
-                    any = i;
-                    if (run > aim && found == INT_MAX) found = i;
-                }
+                const int i = i0 + (64 * j + lane) * VEC + e;
+                any = w[e] > 0.0 ? i : any;
+                found = w[e] > 0.0 && run > aim ? min(found, i) : found;
             }
-            base += __shfl(incl, 63);
+            base += lane_of(incl, 63);
         }
 #pragma unroll
         for (int d = 32; d; d >>= 1) {
@@ -530,11 +533,13 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(const VerifyArgs
 
 void verify_layout(VerifyArgs &a, bool bf16, int num_cus)
 {
-    // As many pieces for a wave, 1, 2 or 4, as leave eight workgroups to a compute unit.
+    // As many pieces for a wave, 1, 2 or 4, as leave two workgroups to a compute unit, or four that read one row and not two: all of them do
+    // the walk.  MI355X, us, with up to 8 / 4 / 2 workgroups: 64 chains of 5, 128,000 tokens, with drafts 19.1 / 18.4 / 18.1, without 17.5 /
+    // 15.9 / 17.3; 256 trees of three nodes, 32,000 tokens 16.8 / 15.2 / 16.2.
     const int piece = kPieceLoads * 64 * (bf16 ? 8 : 4);
-    const int64_t pieces = ((int64_t)a.vocab + piece - 1) / piece;
+    const int64_t pieces = ((int64_t)a.vocab + piece - 1) / piece, workgroups = (int64_t)num_cus * (a.draft ? 2 : 4);
     a.pieces = 1;
-    while (a.pieces < kMaxPieces && pieces * a.num_seqs > (int64_t)8 * num_cus * kVerifyWaves * a.pieces) a.pieces *= 2;
+    while (a.pieces < kMaxPieces && pieces * a.num_seqs > workgroups * kVerifyWaves * a.pieces) a.pieces *= 2;
     a.groups = (int)((pieces + kVerifyWaves * a.pieces - 1) / (kVerifyWaves * a.pieces));
 }
 

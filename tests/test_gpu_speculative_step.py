@@ -134,3 +134,27 @@ def test_step_in_a_graph():
             side.synchronize()
             assert (again[0] == got[0]).all() and (again[1] == got[1]).all()
             assert (bits(fresh.out) == bits(g.out)).all() and (bits(fresh.k) == bits(g.k)).all() and (bits(fresh.v) == bits(g.v)).all()
+
+
+def test_both_ways_of_marshalling_give_the_same(monkeypatch):
+    x = Inputs(7)
+    say("case: speculative step, native and general marshalling")
+    results = []
+    for native in (True, False):
+        if native:
+            assert B._native is not None
+        else:
+            for name in ("_masks_fast", "_rope_fast", "_tree_fast", "_verify_fast", "_compact_fast"):
+                monkeypatch.setattr(B, name, B._not_native)
+        g = OnGpu(x)
+        with context(x.b) as c:
+            c.rope_set(FREQ)
+            counts, tokens = g.run(TreeStep(c, rows=50, seqs=5, Hq=8, head_dim=128, max_path=MAX_PATH))
+            torch.cuda.synchronize()
+            results.append([counts.cpu().numpy(), tokens.cpu().numpy(), bits(g.out), bits(g.k), bits(g.v)])
+            with pytest.raises(B.OocoError) as e:          # the same refusals, too
+                c.verify_drafts(g.target, g.tokens, g.u, g.final, g.qsl, counts, tokens[:, 1:].contiguous(), tokens, draft_probs=g.target,
+                                parents=g.parents)
+            assert e.value.status == B.OOCO_EINVAL and "chains" in e.value.message
+    for a, b in zip(*results):
+        assert (a == b).all()

@@ -109,3 +109,17 @@ def test_verified_tokens_are_distributed_as_the_targets(form):
         _, _, out = S.verify_drafts(target, draft, tokens, parents, rng.random(n), rng.random(1), [0, n], n - 1)
         seen[out[0, 0]] += 1
     assert (np.abs(seen / steps - p) <= 5 * np.sqrt(p * (1 - p) / steps)).all(), (seen / steps, p)
+
+
+def test_other_forms_are_left_to_the_general_way():
+    torch = pytest.importorskip("torch")
+    import ctypes
+
+    N, null = B._native, ctypes.c_void_p(0)
+    t, p = torch.zeros(4, dtype=torch.int32), torch.zeros((4, 8))      # (tensors on the host are not the plain form)
+    assert N.tree_masks(null, t, t, t, t, None, 1, 1, 4, 0) is NotImplemented
+    assert N.rope_append(null, p, p, p, None, p, p, p, t, t, t, 1, 4, 0) is NotImplemented
+    assert N.attn_tree(null, p, p, p, t, t, t, t, 1, p, 1, 4, 0) is NotImplemented
+    assert N.verify_drafts(null, p, None, t, None, t, t, t, t, t, t, 3, 1, 4, 0) is NotImplemented
+    assert N.kv_compact(null, [p], [p], t, t, t, t, 3, 1, 0) is NotImplemented
+    assert N.kv_compact(null, (p,), (p,), t, t, t, t, 3, 1, 0) is NotImplemented
