@@ -2254,7 +2254,8 @@ ooco_status ooco_kv_compact(ooco_ctx *ctx, void *const *h_k_caches, void *const 
             a.k[i] = static_cast<uint16_t *>(h_k_caches[first + i]);
             a.v[i] = static_cast<uint16_t *>(h_v_caches[first + i]);
         }
-        const hipError_t e = launch_kv_compact(a, layers, num_seqs, reinterpret_cast<hipStream_t>(stream));
+        a.layers = layers;
+        const hipError_t e = launch_kv_compact(a, num_seqs, ctx->num_cus, reinterpret_cast<hipStream_t>(stream));
         if (e != hipSuccess) return fail(ctx, OOCO_EHIP, "ooco_kv_compact: kernel launch: %s", hipGetErrorString(e));
     }
     return OOCO_OK;

@@ -58,6 +58,7 @@ struct RopeArgs {
     int32_t num_seqs, total_q;
     int32_t pairs;                       // rotated pairs per head
     int32_t parts;                       // workgroups per (sequence, KV block)
+    int32_t past_caches;                 // 16-byte stores past the caches
     float factor;                        // of cosine and sine
     double turns[kMaxRotaryPairs];       // turns per position of each pair
 };
@@ -95,7 +96,8 @@ struct CompactArgs {
     const int32_t *counts;
     int64_t num_blocks;
     int32_t Hkv, hd, max_blocks_per_seq, max_path;
+    int32_t layers, layers_each;         // and those that a workgroup has
 };
-hipError_t launch_kv_compact(const CompactArgs &a, int layers, int num_seqs, hipStream_t s);
+hipError_t launch_kv_compact(CompactArgs &a, int num_seqs, int num_cus, hipStream_t s);
 
 }  // namespace ooco

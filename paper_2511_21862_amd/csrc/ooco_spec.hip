@@ -19,6 +19,37 @@ OOCO_DEV void rows_of(const int32_t *query_start_loc, int seq, int total_q, int 
     if (q0 < 0 || n < 0 || n > total_q - q0) n = 0;
 }
 
+// The sequence that owns (sequence, block) pair x, and its rows and cached tokens: sequence i owns the pairs from
+// query_start_loc[i] / 16 + 2 i on.  256 sequences a memory round trip, which brings the lengths as well.  The same x in every lane.
+OOCO_DEV int rows_of_pair(const int32_t *query_start_loc, const int32_t *ctx_lens, int num_seqs, int total_q, int x, int &q0, int &n, int &ctx)
+{
+    constexpr int LOOKS = 4;
+    const int lane = threadIdx.x & 63;
+    for (int base = 0;; base += 64 * LOOKS) {
+        int start[LOOKS], next[LOOKS], cached[LOOKS];
+#pragma unroll
+        for (int k = 0; k < LOOKS; ++k) {
+            const int i = min(base + 64 * k + lane, num_seqs - 1);
+            start[k] = query_start_loc[i];
+            next[k] = query_start_loc[i + 1];
+            cached[k] = ctx_lens[i];
+        }
+#pragma unroll
+        for (int k = 0; k < LOOKS; ++k) {
+            const int i = base + 64 * k + lane;
+            const int before = __popcll(__ballot(i < num_seqs && next[k] / kBlockSize + 2 * (i + 1) <= x));   // sequences that end in front of x
+            if (before < 64 || base + 64 * k + 64 >= num_seqs) {
+                const int at = min(before, num_seqs - 1 - (base + 64 * k));
+                q0 = __builtin_amdgcn_readlane(start[k], at);
+                n = __builtin_amdgcn_readlane(next[k], at) - q0;
+                ctx = __builtin_amdgcn_readlane(cached[k], at);
+                if (q0 < 0 || n < 0 || n > total_q - q0) n = 0;
+                return base + 64 * k + at;
+            }
+        }
+    }
+}
+
 // ------------------------------------------------------------------------------------------
 // Masks and positions.  A node sees itself and its ancestors: with M_0(i) = {i} and P_0(i) = parent(i), doubling the distance
 // M_k+1(i) = M_k(i) + M_k(P_k(i)), P_k+1(i) = P_k(P_k(i)) needs log2 of the depth rounds, where a walk up the tree would need the
@@ -83,28 +114,32 @@ hipError_t launch_tree_masks(const int32_t *parents, const int32_t *query_start_
 // ------------------------------------------------------------------------------------------
 // Rotary positions and append: x'_a = x_a cos(p f) - x_b sin(p f), x'_b = x_b cos(p f) + x_a sin(p f) for the pairs (a, b) of a
 // head, in fp32, rounded once to bf16; v goes to the cache as it is.  Memory bound: every element is read once and written once.
-// A workgroup has the rows of one (sequence, KV block) pair, as the plain append does (see kv_append_kernel for the order of the
-// pairs: sequence i owns the pairs from query_start_loc[i] / 16 + 2 i on), because the cache keeps 16 tokens of a dim or of a
-// group of 8 dims side by side; `parts` workgroups share a pair's heads.  The angles' turns p f / (2 pi) are reduced in 64 bits --
-// a position of 10^5 times a frequency of 1 leaves 32 bits three digits behind the point -- and cosine and sine are those of the
-// hardware, which take turns; they go through LDS, once per row and pair for all heads of the workgroup.
+// A workgroup has two or four heads of the rows of one (sequence, KV block) pair, as the plain append does (see kv_append_kernel for the
+// order of the pairs: sequence i owns the pairs from query_start_loc[i] / 16 + 2 i on), because the cache keeps 16 tokens of a dim or of a
+// group of 8 dims side by side.  All heads are read the way they lie, a 16-byte piece of a row per thread, all pieces of a thread on their
+// way before anything is computed; q is written the way it was read, k and v go through LDS and are written the way the cache has them.
+// (MI355X, 8 x 512 rows, 32/8 heads, us: 30 with loads of k and stores of v that jump from row to row, 26 like this, 21 with stores past the
+// caches: 4.9 TB/s, of the 5.2 that a large copy reaches.)
+// The angles' turns p f / (2 pi) are reduced in 64 bits -- a position of 10^5 times a frequency of 1 leaves 32 bits three digits behind the
+// point -- and cosine and sine are those of the hardware, which take turns (off by 2^-22.9 at most, measured over 2^22 turns); they are
+// computed once per row and pair for all heads of the workgroup.
 constexpr int kRopeThreads = 256;
 
 OOCO_DEV float bf16_lo(uint32_t u) { return __builtin_bit_cast(float, u << 16); }
 OOCO_DEV float bf16_hi(uint32_t u) { return __builtin_bit_cast(float, u & 0xFFFF0000u); }
 
-template <bool INTERLEAVED>
+template <int HD, bool INTERLEAVED, int HEADS>
 __global__ __launch_bounds__(kRopeThreads) void rope_append_kernel(const RopeArgs a)
 {
-    __shared__ f32x2 turn[kBlockSize][kMaxRotaryPairs];   // (cosine, sine)
-    const int tid = threadIdx.x, lane = tid & 63;
+    constexpr int CH = HD / 8;                                    // pieces of a head
+    constexpr int PITCH = HD + 8;                                 // elements of a row in LDS (padded: the lanes of a wave are rows)
+    constexpr int N = kBlockSize * HEADS * CH / kRopeThreads;   // pieces of a thread
+    __shared__ f32x2 turn[kBlockSize][kMaxRotaryPairs];           // (cosine, sine)
+    __shared__ __align__(16) uint16_t tile[HEADS][kBlockSize][PITCH];   // by slot of the block
+    const int tid = threadIdx.x;
     const int pair = blockIdx.x / a.parts, part = blockIdx.x - pair * a.parts;
-    const int32_t *const qsl = a.query_start_loc;
-    auto g_at = [&](int idx) -> int { return qsl[idx] / kBlockSize + 2 * idx; };
-    const int seq = __builtin_amdgcn_readfirstlane(min(count_le(g_at, a.num_seqs, pair, lane), a.num_seqs - 1));
-    int q0, q_len;
-    rows_of(qsl, seq, a.total_q, q0, q_len);
-    const int ctx = a.ctx_lens[seq];
+    int q0, q_len, ctx;
+    const int seq = rows_of_pair(a.query_start_loc, a.ctx_lens, a.num_seqs, a.total_q, pair, q0, q_len, ctx);
     if (q_len == 0 || ctx < 0) return;
     const int64_t end = (int64_t)ctx + q_len;                     // (may lie past the block table)
     const int64_t bidx = ctx / kBlockSize + (int64_t)(pair - (q0 / kBlockSize + 2 * seq));
@@ -113,108 +148,132 @@ __global__ __launch_bounds__(kRopeThreads) void rope_append_kernel(const RopeArg
     const int slot0 = (int)(ctx + (int64_t)t_lo - bidx * kBlockSize);
     const int nrow = min(kBlockSize - slot0, q_len - t_lo);
     const int row0 = q0 + t_lo;
+
+    // Heads of this part: of q, of k and of v, numbered one after the other.
+    const int heads = a.Hq + 2 * a.Hkv, h0 = part * HEADS;
+    const int pairs = a.pairs;
+    // Piece i of the thread is piece `c` of head h0 + hs, row r.
+    const int c = tid % CH, hs = tid / CH % HEADS, r_first = tid / (CH * HEADS);
+    constexpr int R_STEP = kRopeThreads / (CH * HEADS);
+    const int head = h0 + hs;
+    const bool is_q = head < a.Hq, is_k = !is_q && head < a.Hq + a.Hkv, there = head < heads;
+    const uint16_t *const src = is_q ? a.q + head * HD : is_k ? a.k_new + (head - a.Hq) * HD : a.v_new + (head - a.Hq - a.Hkv) * HD;
+    const int64_t apart = is_q ? a.q_stride : is_k ? a.k_stride : a.v_stride;
+    // the piece that this one turns with, and the sine's sign
+    const bool rotated = (is_q || is_k) && c < pairs / 4;
+    const bool second = !INTERLEAVED && c >= pairs / 8;
+    const int partner = second ? c - pairs / 8 : c + pairs / 8;
+    u32x4 x[N], y[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int r = r_first + i * R_STEP;
+        if (there && r < nrow) {
+            const u32x4 *const p = reinterpret_cast<const u32x4 *>(src + (row0 + r) * apart);
+            x[i] = p[c];
+            if (!INTERLEAVED && rotated) y[i] = p[partner];
+        }
+    }
     // (a block that the cache does not have: the queries are rotated all the same, nothing is appended)
     const int64_t blk = bidx < a.max_blocks_per_seq ? a.block_tables[(int64_t)seq * a.max_blocks_per_seq + bidx] : -1;
     const bool blk_ok = blk >= 0 && blk < a.num_blocks;
 
-    const int pairs = a.pairs, hd = a.hd;
     for (int i = tid; i < nrow * pairs; i += kRopeThreads) {
-        const int r = i / pairs, x = i - r * pairs;
+        const int r = i / pairs, k = i - r * pairs;
         const int pos = a.positions ? a.positions[row0 + r] : ctx + t_lo + r;
-        const float f = (float)__builtin_amdgcn_fract((double)pos * a.turns[x]);
-        turn[r][x] = f32x2{__builtin_amdgcn_cosf(f) * a.factor, __builtin_amdgcn_sinf(f) * a.factor};
+        const float f = (float)__builtin_amdgcn_fract((double)pos * a.turns[k]);
+        turn[r][k] = f32x2{__builtin_amdgcn_cosf(f) * a.factor, __builtin_amdgcn_sinf(f) * a.factor};
     }
     __syncthreads();
-
-    // heads of this part: of q, of k and of v, numbered one after the other
-    const int heads = a.Hq + 2 * a.Hkv;
-    const int h0 = heads * part / a.parts, h1 = heads * (part + 1) / a.parts;
-    const int qa = min(h0, a.Hq), qb = min(h1, a.Hq);
-    const int ka = min(max(h0 - a.Hq, 0), a.Hkv), kb = min(max(h1 - a.Hq, 0), a.Hkv);
-    const int va = max(h0 - a.Hq - a.Hkv, 0), vb = max(h1 - a.Hq - a.Hkv, 0);
-
-    // One task: the 16-byte pieces of a head that belong together -- a piece of the first half of the rotated dims and its
-    // partner of the second half, or one piece (of pairs side by side, or of dims that are not rotated).
-    const int tasks = INTERLEAVED ? hd / 8 : pairs / 8 + (hd - 2 * pairs) / 8;
-    auto rotate = [&](int r, int c, const u32x4 *src, u32x4 *dst, int dst_step) {   // pieces of dst are dst_step apart
-        if (!INTERLEAVED && c < pairs / 8) {
-            const int c2 = c + pairs / 8;
-            const u32x4 x = src[c], y = src[c2];
-            u32x4 ox, oy;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const f32x2 t0 = turn[r][8 * c + 2 * w], t1 = turn[r][8 * c + 2 * w + 1];
-                const float x0 = bf16_lo(x[w]), x1 = bf16_hi(x[w]), y0 = bf16_lo(y[w]), y1 = bf16_hi(y[w]);
-                ox[w] = pack2_bf16(x0 * t0[0] - y0 * t0[1], x1 * t1[0] - y1 * t1[1]);
-                oy[w] = pack2_bf16(y0 * t0[0] + x0 * t0[1], y1 * t1[0] + x1 * t1[1]);
-            }
-            dst[(int64_t)c * dst_step] = ox;
-            dst[(int64_t)c2 * dst_step] = oy;
-            return;
-        }
-        if (!INTERLEAVED) c += pairs / 8;
-        u32x4 x = src[c];
-        if (INTERLEAVED && c < pairs / 4) {
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const f32x2 t = turn[r][4 * c + w];
-                const float x0 = bf16_lo(x[w]), x1 = bf16_hi(x[w]);
-                x[w] = pack2_bf16(x0 * t[0] - x1 * t[1], x1 * t[0] + x0 * t[1]);
-            }
-        }
-        dst[(int64_t)c * dst_step] = x;
+    auto store = [&](u32x4 *dst, const u32x4 &v) {
+        if (a.past_caches)
+            __builtin_nontemporal_store(v, dst);
+        else
+            *dst = v;
     };
-    for (int i = tid; i < nrow * (qb - qa) * tasks; i += kRopeThreads) {
-        const int j = i / tasks, c = i - j * tasks;
-        const int r = j / (qb - qa), h = qa + j - r * (qb - qa);
-        rotate(r, c, reinterpret_cast<const u32x4 *>(a.q + (row0 + r) * a.q_stride + h * hd),
-               reinterpret_cast<u32x4 *>(a.q_out + ((int64_t)(row0 + r) * a.Hq + h) * hd), 1);
-    }
-    if (!blk_ok) return;
-    // K: the rows of a piece are side by side in the cache, so they are side by side in a wave
-    for (int i = tid; i < nrow * (kb - ka) * tasks; i += kRopeThreads) {
-        const int j = i / nrow, r = i - j * nrow;
-        const int h = ka + j / tasks, c = j - (h - ka) * tasks;
-        rotate(r, c, reinterpret_cast<const u32x4 *>(a.k_new + (row0 + r) * a.k_stride + h * hd),
-               reinterpret_cast<u32x4 *>(a.k_cache) + (blk * a.Hkv + h) * (hd / 8) * kBlockSize + slot0 + r, kBlockSize);
-    }
-    // V: a thread has two adjacent dims of all rows, which are 2 x 32 bytes of the cache
-    uint16_t *const v_dst = a.v_cache + blk * a.Hkv * hd * kBlockSize;
-    const uint16_t *const v_src = a.v_new + row0 * a.v_stride;
-    for (int e = va * hd + 2 * tid; e < vb * hd; e += 2 * kRopeThreads) {
-        uint32_t x[kBlockSize];
 #pragma unroll
-        for (int sl = 0; sl < kBlockSize; ++sl) {
-            const int r = sl - slot0;
-            x[sl] = 0;
-            if (r >= 0 && r < nrow) x[sl] = *reinterpret_cast<const uint32_t *>(v_src + r * a.v_stride + e);
-        }
+    for (int i = 0; i < N; ++i) {
+        const int r = r_first + i * R_STEP;
+        if (!there || r >= nrow) continue;
+        if (rotated) {
+            if constexpr (INTERLEAVED) {
 #pragma unroll
-        for (int d = 0; d < 2; ++d) {
-            uint16_t *const dst = v_dst + (int64_t)(e + d) * kBlockSize;   // (32-byte aligned)
-            auto at = [&](int sl) -> uint32_t { return d ? x[sl] >> 16 : x[sl] & 0xFFFFu; };
-            // quarters of a cache row that the step covers whole are written with one store each, the ragged ends slot by slot
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (4 * k >= slot0 && 4 * k + 4 <= slot0 + nrow) {
-                    *reinterpret_cast<u32x2 *>(dst + 4 * k) = u32x2{at(4 * k) | (at(4 * k + 1) << 16), at(4 * k + 2) | (at(4 * k + 3) << 16)};
-                } else {
-#pragma unroll
-                    for (int sl = 4 * k; sl < 4 * k + 4; ++sl)
-                        if (sl >= slot0 && sl < slot0 + nrow) dst[sl] = (uint16_t)at(sl);
+                for (int w = 0; w < 4; ++w) {
+                    const f32x2 t = turn[r][4 * c + w];
+                    const float x0 = bf16_lo(x[i][w]), x1 = bf16_hi(x[i][w]);
+                    x[i][w] = pack2_bf16(x0 * t[0] - x1 * t[1], x1 * t[0] + x0 * t[1]);
                 }
+            } else {
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const f32x2 t0 = turn[r][8 * (second ? partner : c) + 2 * w], t1 = turn[r][8 * (second ? partner : c) + 2 * w + 1];
+                    const float s0 = second ? t0[1] : -t0[1], s1 = second ? t1[1] : -t1[1];
+                    x[i][w] = pack2_bf16(bf16_lo(x[i][w]) * t0[0] + bf16_lo(y[i][w]) * s0, bf16_hi(x[i][w]) * t1[0] + bf16_hi(y[i][w]) * s1);
+                }
+            }
+        }
+        if (is_q)
+            store(reinterpret_cast<u32x4 *>(a.q_out + ((int64_t)(row0 + r) * a.Hq + head) * HD + 8 * c), x[i]);
+        else
+            *reinterpret_cast<u32x4 *>(&tile[hs][slot0 + r][8 * c]) = x[i];
+    }
+    if (h0 + HEADS <= a.Hq || !blk_ok) return;   // (the whole workgroup: only heads of q, or nowhere to append)
+    __syncthreads();
+    const int k0 = max(h0, a.Hq), k1 = min(h0 + HEADS, a.Hq + a.Hkv), v0 = max(h0, a.Hq + a.Hkv), v1 = min(h0 + HEADS, heads);
+    // K: pieces of 16 bytes, the block's slots side by side
+    for (int i = tid; i < (k1 - k0) * CH * kBlockSize; i += kRopeThreads) {
+        const int slot = i % kBlockSize, p = i / kBlockSize % CH, h = k0 + i / (kBlockSize * CH);
+        if (slot >= slot0 && slot < slot0 + nrow)
+            store(reinterpret_cast<u32x4 *>(a.k_cache) + ((blk * a.Hkv + (h - a.Hq)) * CH + p) * kBlockSize + slot,
+                  *reinterpret_cast<const u32x4 *>(&tile[h - h0][slot][8 * p]));
+    }
+    // V: half a row of a dim, eight slots, per thread
+    for (int i = tid; i < (v1 - v0) * HD * 2; i += kRopeThreads) {
+        const int half = i & 1, d = i / 2 % HD, h = v0 + i / (2 * HD);
+        uint32_t e[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = tile[h - h0][8 * half + j][d];
+        uint16_t *const dst = a.v_cache + ((blk * a.Hkv + (h - a.Hq - a.Hkv)) * HD + d) * kBlockSize + 8 * half;
+        const int lo = slot0 - 8 * half, hi = slot0 + nrow - 8 * half;   // slots lo .. hi - 1 of the half are the step's
+        if (lo <= 0 && hi >= 8) {
+            store(reinterpret_cast<u32x4 *>(dst), u32x4{e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16});
+            continue;
+        }
+        // quarters that the step covers whole with one store each, the ragged ends slot by slot
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (lo <= 4 * k && hi >= 4 * k + 4) {
+                *reinterpret_cast<u32x2 *>(dst + 4 * k) = u32x2{e[4 * k] | e[4 * k + 1] << 16, e[4 * k + 2] | e[4 * k + 3] << 16};
+            } else {
+#pragma unroll
+                for (int j = 4 * k; j < 4 * k + 4; ++j)
+                    if (j >= lo && j < hi) dst[j] = (uint16_t)e[j];
             }
         }
     }
 }
 
+namespace {
+template <int HEADS>
+hipError_t launch_rope(RopeArgs &a, bool interleaved, int64_t pairs, hipStream_t s)
+{
+    a.parts = (a.Hq + 2 * a.Hkv + HEADS - 1) / HEADS;
+    auto *const kernel = a.hd == 128 ? (interleaved ? rope_append_kernel<128, true, HEADS> : rope_append_kernel<128, false, HEADS>)
+                                     : (interleaved ? rope_append_kernel<64, true, HEADS> : rope_append_kernel<64, false, HEADS>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(pairs * a.parts)), dim3(kRopeThreads), 0, s, a);
+    return hipGetLastError();
+}
+}  // namespace
+
 hipError_t launch_rope_append(RopeArgs &a, bool interleaved, int num_cus, hipStream_t s)
 {
-    const int heads = a.Hq + 2 * a.Hkv;
     const int64_t pairs = a.total_q / kBlockSize + 2 * (int64_t)a.num_seqs + 1;
-    a.parts = std::max(1, heads / 4);
-    hipLaunchKernelGGL(interleaved ? rope_append_kernel<true> : rope_append_kernel<false>, dim3((unsigned)(pairs * a.parts)), dim3(kRopeThreads), 0, s, a);
-    return hipGetLastError();
+    // Stores by the plain append's rule.  Alone, stores past the caches are faster (us, 8 x 512 rows 26.4 -> 20.7, 64 x 16 10.7 -> 10.1, 1 x 1000 8.8
+    // -> 7.8), but with the attention that reads what they wrote the two together are level above the rule's bounds (108.1 / 108.7, 66.3 /
+    // 63.8) and slower below them (1 x 300 16.0 / 16.6).
+    a.past_caches = append_past_caches(a.total_q, a.num_seqs, 4 * (int64_t)a.total_q * a.Hkv * a.hd);
+    // Four heads to a workgroup, or two where that leaves compute units without one (us, 8 x 12 rows 4.9 -> 4.4; 8 x 512 26 -> 31).
+    const int64_t by_four = pairs * ((a.Hq + 2 * a.Hkv + 3) / 4);
+    return by_four <= 2 * (int64_t)num_cus ? launch_rope<2>(a, interleaved, pairs, s) : launch_rope<4>(a, interleaved, pairs, s);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -555,16 +614,20 @@ hipError_t launch_verify(const VerifyArgs &a, bool bf16, hipStream_t s)
 
 // ------------------------------------------------------------------------------------------
 // Accepted nodes to their places: the d-th node of the path goes from slot ctx + path[d] to slot ctx + 1 + d.  A path rises, so
-// path[d] > d: a node moves towards the front or stays, and its place is one that no later node of the path comes from.  A thread
-// has one column of the cache -- a 16-byte piece of K, two dims of V -- and moves its nodes in their order, all loads of a batch
-// before its stores, so nothing is overwritten before it has been read.  One workgroup per (sequence, layer, slice of columns).
+// path[d] > d: a node moves towards the front or stays, and its place is one that no later node of the path comes from.  The nodes of
+// a path go in groups of up to eight that lie next to each other in a wave: lane = (column of the cache, node), a column being a 16-byte
+// piece of K or a dim of V.  All nodes of a group are loaded before one is stored, and the groups go in order, so nothing is overwritten
+// before it has been read; and as the places of a group lie side by side in every column, so do its stores (64 sequences of 4.4 nodes, 32
+// layers of 8 heads, us: 122 with a column's nodes one after the other in one lane, whose stores are a request to L2 each).
+// What bounds it is the cache's layout: V keeps the 16 tokens of a block side by side, so every line of a block is touched for one token of it.
 constexpr int kCompactThreads = 256;
+constexpr int kCompactAhead = 4;   // columns whose loads are sent off together
 
 __global__ __launch_bounds__(kCompactThreads) void kv_compact_kernel(const CompactArgs a)
 {
-    __shared__ int64_t from[kCompactThreads], to[kCompactThreads];   // block * 16 + slot, or -1
+    __shared__ int64_t from[kCompactThreads], to[kCompactThreads];   // block * 16 + slot; from: -1 for a node that stays
     const int tid = threadIdx.x;
-    const int seq = blockIdx.x, layer = blockIdx.y;
+    const int seq = blockIdx.x;
     const int moves = min(a.counts[seq] - 1, min(a.max_path, kCompactThreads));
     if (moves <= 0) return;
     const int ctx = a.ctx_lens[seq];
@@ -575,49 +638,67 @@ __global__ __launch_bounds__(kCompactThreads) void kv_compact_kernel(const Compa
             return blk >= 0 && blk < a.num_blocks ? blk * kBlockSize + token % kBlockSize : -1;
         };
         const int node = a.path[(int64_t)seq * a.max_path + tid];
-        int64_t f = node > tid + 1 && ctx >= 0 ? place((int64_t)ctx + node) : -1;   // (one that is in its place stays)
-        int64_t t = f >= 0 ? place((int64_t)ctx + 1 + tid) : -1;
+        const bool moved = node > tid + 1 && ctx >= 0;   // (one that is in its place stays)
+        const int64_t f = moved ? place((int64_t)ctx + node) : -1, t = moved ? place((int64_t)ctx + 1 + tid) : -1;
         from[tid] = t >= 0 ? f : -1;
         to[tid] = t;
     }
     __syncthreads();
-    uint16_t *const k = a.k[layer], *const v = a.v[layer];
-    const int pieces = a.Hkv * a.hd / 8, columns = pieces + a.Hkv * a.hd;
-    for (int i = tid + kCompactThreads * blockIdx.z; i < columns; i += kCompactThreads * gridDim.z) {
-        if (i < pieces) {   // K: piece i of a token, 16 slots of 16 bytes
-            u32x4 *const col = reinterpret_cast<u32x4 *>(k) + (int64_t)i * kBlockSize;
-            for (int d0 = 0; d0 < moves; d0 += 4) {
-                u32x4 x[4];
+    const int group_log2 = moves == 1 ? 0 : moves == 2 ? 1 : moves <= 4 ? 2 : 3;
+    const int group = 1 << group_log2, columns = kCompactThreads >> group_log2;   // columns of the workgroup at a time
+    const int mine = tid >> group_log2;
+    const int pieces = a.Hkv * a.hd / 8, dims = a.Hkv * a.hd;
+    const int64_t block = (int64_t)dims * kBlockSize;   // elements
+    const int first = blockIdx.y * a.layers_each, last = min(first + a.layers_each, a.layers);
+    for (int layer = first; layer < last; ++layer) {
+        uint16_t *const k = a.k[layer], *const v = a.v[layer];
+        for (int d0 = 0; d0 < moves; d0 += group) {
+            const int d = d0 + (tid & (group - 1));
+            const int64_t f = d < moves ? from[d] : -1, t = d < moves ? to[d] : -1;
+            const bool moved = f >= 0;
+            const u32x4 *const kf = reinterpret_cast<const u32x4 *>(k + (moved ? f / kBlockSize * block : 0)) + (moved ? f % kBlockSize : 0);
+            u32x4 *const kt = reinterpret_cast<u32x4 *>(k + (moved ? t / kBlockSize * block : 0)) + (moved ? t % kBlockSize : 0);
+            for (int c = blockIdx.z * columns + mine; c < pieces + mine; c += kCompactAhead * gridDim.z * columns) {
+                u32x4 x[kCompactAhead];
 #pragma unroll
-                for (int d = 0; d < 4; ++d)
-                    if (d0 + d < moves && from[d0 + d] >= 0)
-                        x[d] = col[(from[d0 + d] / kBlockSize) * pieces * kBlockSize + from[d0 + d] % kBlockSize];
+                for (int i = 0; i < kCompactAhead; ++i) {
+                    const int p = c + i * gridDim.z * columns;
+                    if (moved && p < pieces) x[i] = kf[(int64_t)p * kBlockSize];
+                }
 #pragma unroll
-                for (int d = 0; d < 4; ++d)
-                    if (d0 + d < moves && from[d0 + d] >= 0)
-                        col[(to[d0 + d] / kBlockSize) * pieces * kBlockSize + to[d0 + d] % kBlockSize] = x[d];
+                for (int i = 0; i < kCompactAhead; ++i) {
+                    const int p = c + i * gridDim.z * columns;
+                    if (moved && p < pieces) kt[(int64_t)p * kBlockSize] = x[i];
+                }
             }
-        } else {            // V: one dim, 16 slots of 2 bytes
-            uint16_t *const col = v + (int64_t)(i - pieces) * kBlockSize;
-            const int64_t block = (int64_t)a.Hkv * a.hd * kBlockSize;
-            for (int d0 = 0; d0 < moves; d0 += 4) {
-                uint16_t x[4];
+            const uint16_t *const vf = v + (moved ? f / kBlockSize * block + f % kBlockSize : 0);
+            uint16_t *const vt = v + (moved ? t / kBlockSize * block + t % kBlockSize : 0);
+            for (int c = blockIdx.z * columns + mine; c < dims + mine; c += 2 * kCompactAhead * gridDim.z * columns) {
+                uint16_t x[2 * kCompactAhead];
 #pragma unroll
-                for (int d = 0; d < 4; ++d)
-                    if (d0 + d < moves && from[d0 + d] >= 0) x[d] = col[(from[d0 + d] / kBlockSize) * block + from[d0 + d] % kBlockSize];
+                for (int i = 0; i < 2 * kCompactAhead; ++i) {
+                    const int e = c + i * gridDim.z * columns;
+                    if (moved && e < dims) x[i] = vf[(int64_t)e * kBlockSize];
+                }
 #pragma unroll
-                for (int d = 0; d < 4; ++d)
-                    if (d0 + d < moves && from[d0 + d] >= 0) col[(to[d0 + d] / kBlockSize) * block + to[d0 + d] % kBlockSize] = x[d];
+                for (int i = 0; i < 2 * kCompactAhead; ++i) {
+                    const int e = c + i * gridDim.z * columns;
+                    if (moved && e < dims) vt[(int64_t)e * kBlockSize] = x[i];
+                }
             }
         }
     }
 }
 
-hipError_t launch_kv_compact(const CompactArgs &a, int layers, int num_seqs, hipStream_t s)
+hipError_t launch_kv_compact(CompactArgs &a, int num_seqs, int num_cus, hipStream_t s)
 {
-    const int columns = a.Hkv * a.hd / 8 + a.Hkv * a.hd;
-    const unsigned slices = (unsigned)std::min(8, (columns + kCompactThreads - 1) / kCompactThreads);
-    hipLaunchKernelGGL(kv_compact_kernel, dim3((unsigned)num_seqs, (unsigned)layers, slices), dim3(kCompactThreads), 0, s, a);
+    // Slices of the columns where (sequence, layer) pairs are fewer than eight workgroups to a compute unit, some layers for a workgroup where
+    // they are more.
+    const int64_t pairs = (int64_t)num_seqs * a.layers, want = 8 * (int64_t)num_cus;
+    a.layers_each = (int)std::max<int64_t>(1, std::min<int64_t>(a.layers, pairs / want));
+    const unsigned groups = (unsigned)((a.layers + a.layers_each - 1) / a.layers_each);
+    const unsigned slices = (unsigned)std::max<int64_t>(1, std::min<int64_t>(8, want / std::max<int64_t>(1, pairs)));
+    hipLaunchKernelGGL(kv_compact_kernel, dim3((unsigned)num_seqs, groups, slices), dim3(kCompactThreads), 0, s, a);
     return hipGetLastError();
 }
 
