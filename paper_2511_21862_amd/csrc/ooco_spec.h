@@ -27,6 +27,7 @@ struct TreeArgs {
     int32_t max_blocks_per_seq;
     int32_t num_seqs, total_q, words;
     int32_t runs_log2;          // runs of the line: 1 << runs_log2 workgroups
+    int64_t halve_below;        // half the runs on a line of fewer steps
     int32_t tile_rows;          // rows of the widest tile
     int32_t short_line;         // up to 64 sequences, and a line of 31 bits
     float scale_log2e;          // softmax scale * log2(e)

@@ -25,7 +25,6 @@
 namespace ooco {
 
 constexpr int kTreeStep = 128;               // tokens of a step
-constexpr int kMinRun = 1;                   // steps of a run, at least
 constexpr int kMergeInts = 5;
 constexpr int kMergeSlices = 8;
 constexpr int kMergeThreads = 256;
@@ -83,14 +82,18 @@ OOCO_DEV TreeSeq tree_seq_at(const TreeArgs &p, int seq)
     return tree_seq(p, qsl[seq], qsl[seq + 1], ctx[seq]);
 }
 
-// Runs of the line: run w = [first(w), first(w + 1)).  No run is empty but those behind `count`.
+// Runs of the line: run w = [first(w), first(w + 1)).  No run is empty but those behind the last.  As many as there are workgroups, or half as
+// many (see launch); on a line shorter than that a run for each step, which takes the shortest time.
 struct TreeRuns {
     int64_t total;
     int log2;
-    bool split;      // the line is cut into all runs there are, else into runs of kMinRun steps
-    OOCO_DEV TreeRuns(int64_t total_, int log2_) : total(total_), log2(log2_), split(total_ >= ((int64_t)kMinRun << log2_)) {}
-    OOCO_DEV int64_t first(int w) const { return split ? (total * w) >> log2 : min(total, (int64_t)w * kMinRun); }
-    OOCO_DEV int holding(int64_t x) const { return split ? (int)quotient(((x + 1) << log2) - 1, total) : (int)(x / kMinRun); }
+    bool split;      // the line is cut into 1 << log2 runs, else into runs of one step
+    OOCO_DEV TreeRuns(const TreeArgs &p, int64_t total_)
+        : total(total_), log2(total_ < p.halve_below ? p.runs_log2 - 1 : p.runs_log2), split(total_ >= ((int64_t)1 << log2))
+    {
+    }
+    OOCO_DEV int64_t first(int w) const { return split ? (w >> log2 ? total : (total * w) >> log2) : min(total, (int64_t)w); }
+    OOCO_DEV int holding(int64_t x) const { return split ? (int)quotient(((x + 1) << log2) - 1, total) : (int)x; }
 };
 
 // The line: its length, and the sequence that holds position at(total) of it, with the position of that sequence's first step.
@@ -325,20 +328,20 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_kernel(const TreeArgs p)
     const int col = lane & 31, h = lane >> 5;
     const int g = p.g;
     // Runs next to each other on the line are on one XCD (workgroup b runs on XCD b % 8): the tiles of one sequence and kv head walk the
-    // same tokens at about the same time, and share an L2 (512 columns on 14,000 tokens, us: 286 -> 255).  A line of fewer runs than there
-    // are workgroups is spread over the XCDs.
+    // same tokens at about the same time, and share an L2 (512 columns on 14,000 tokens, us: 286 -> 255).  A line of runs of one
+    // step is spread over the XCDs.
     int w = blockIdx.x, seq = 0;
     int64_t start = 0;
     TreeSeq s = {};
     const int64_t total = tree_locate<NT>(
         p,
         [&](int64_t t) {
-            const TreeRuns r(t, p.runs_log2);
-            if (r.split && p.runs_log2 >= 3) w = (int)((blockIdx.x & 7) << (p.runs_log2 - 3)) + (int)(blockIdx.x >> 3);
+            const TreeRuns r(p, t);
+            if (r.split && r.log2 >= 3 && w >> r.log2 == 0) w = (w & 7) << (r.log2 - 3) | w >> 3;
             return r.first(w);
         },
         seq, start, s);
-    const TreeRuns runs(total, p.runs_log2);
+    const TreeRuns runs(p, total);
     const int64_t lo = runs.first(w), hi = runs.first(w + 1);
     int32_t *const merge = p.merges + (int64_t)w * kMergeInts;
     if (lo >= hi) {
@@ -759,6 +762,13 @@ hipError_t launch(TreeArgs &a, void *ws, hipStream_t s)
     a.tile_rows = 32 * NW / a.g;
     const int64_t tiles = a.total_q / a.tile_rows + (int64_t)a.num_seqs, steps = (int64_t)a.max_blocks_per_seq * kBlockSize / kTreeStep + 1;
     a.short_line = a.num_seqs <= 64 && (double)tiles * (double)a.Hkv * (double)steps < 2147483647.0;
+    // One workgroup of four waves to a compute unit, and so half the runs, cuts fewer units, but waits with nothing else to do.  With
+    // 32 columns, where its loads are a turn ahead, it is the faster whenever two to a compute unit would have to cut most units (fewer units than runs,
+    // by the average sequence), else on a line of less than four steps a run.  MI355X, us, all runs / half, 32/8 heads: 8 nodes, 8 sequences of 2000 tokens
+    // 27.2 / 22.8, 32 of 4096 98.6 / 90.0, 16 of 20,000 215 / 206, 64 of 100 .. 1000 (as many units as runs) 46.9 / 52.3; 32 sequences of
+    // 32 nodes on 600 tokens (2.5 steps) 45.2 / 32.9, 16 of 24 nodes on 1000 .. 4000 (5) 55.4 / 57.9.
+    const int64_t per_seq = ((int64_t)a.total_q + a.num_seqs - 1) / a.num_seqs, units = ((per_seq + a.tile_rows - 1) / a.tile_rows) * a.Hkv * a.num_seqs;
+    a.halve_below = NW == 8 || runs < 2 || units >= (int64_t)runs ? 0 : per_seq * a.g <= 32 ? INT64_MAX : (int64_t)4 << a.runs_log2;
     a.part_acc = static_cast<float *>(ws);
     a.part_ml = a.part_acc + (size_t)2 * runs * (32 * NW) * HD;
     a.merges = reinterpret_cast<int32_t *>(a.part_ml + (size_t)2 * runs * (32 * NW) * 2);
