@@ -32,7 +32,7 @@ struct TreeArgs {
     int32_t short_line;         // up to 64 sequences, and a line of 31 bits
     float scale_log2e;          // softmax scale * log2(e)
 };
-// Waves of a workgroup: 4 or 8.
+// Blocks of 32 columns of the widest tile: 2 (four waves that share the tokens), 4 or 8 (a wave each).
 int tree_waves(int total_q, int num_seqs, int Hkv, int g, int max_blocks_per_seq, int num_cus);
 // Runs (a power of two) that a workspace of ws_bytes allows on num_cus compute units, as their logarithm; < 0: none.
 int tree_runs_log2(int waves, int hd, int num_cus, size_t ws_bytes);

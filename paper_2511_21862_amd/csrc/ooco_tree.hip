@@ -15,6 +15,7 @@
 //                     shared, so nobody waits for anybody, and a compute unit has 128 KiB on their way
 //   more              K and V of 64 tokens at a time go through LDS by direct loads into the other of two buffers
 //   32 for each wave  the products of 32 tokens run beside the exponentials of 32 others (see region)
+// Few sequences of up to 64 columns have a kernel of their own, in which a wave's registers hold all columns (see tree_stream_kernel).
 #include "ooco_device.h"
 #include "ooco_internal.h"
 #include "ooco_spec.h"
@@ -175,6 +176,25 @@ OOCO_DEV int64_t tree_locate(const TreeArgs &p, At at, int &seq, int64_t &start,
     return uniform(total);
 }
 
+// The workgroup's run, w, and the sequence that it begins in, with the position of that sequence's first step.
+// Runs next to each other on the line are on one XCD (workgroup b runs on XCD b % 8): the tiles of one sequence and kv head walk the same
+// tokens at about the same time, and share an L2 (512 columns on 14,000 tokens, us: 286 -> 255).  A line of runs of one step is spread over
+// the XCDs.
+template <int NT>
+OOCO_DEV TreeRuns tree_run(const TreeArgs &p, int &w, int &seq, int64_t &start, TreeSeq &s)
+{
+    w = blockIdx.x;
+    const int64_t total = tree_locate<NT>(
+        p,
+        [&](int64_t t) {
+            const TreeRuns r(p, t);
+            if (r.split && r.log2 >= 3 && w >> r.log2 == 0) w = (w & 7) << (r.log2 - 3) | w >> 3;
+            return r.first(w);
+        },
+        seq, start, s);
+    return TreeRuns(p, total);
+}
+
 // What a wave does with 32 tokens, whichever way they come: its 32 query columns' share of the softmax and of the output.
 template <int HD>
 struct TreeWave {
@@ -267,6 +287,44 @@ struct TreeWave {
     }
 };
 
+// A column of a unit: the n waves that have it left sums and weights in LDS, `apart` rows from each other.  NT / 32 threads take it, to its
+// place in the output or, of a unit that runs have cut, among the partial results.
+template <int HD, int NT, int ROW>
+OOCO_DEV void tree_column(const TreeArgs &p, const float (*slab)[ROW], const float (*stat)[2], int at, int apart, int n, bool whole, int64_t part,
+                          int row0, int col, int kvh)
+{
+    constexpr int TC = NT / 32, PER = HD / TC;   // threads of a column, dims of each
+    const int d = threadIdx.x % TC * PER;
+    float M = -INFINITY, l = 0.f;
+    for (int k = 0; k < n; ++k) M = fmaxf(M, stat[at + k * apart][0]);
+    f32x4 acc[PER / 4];
+#pragma unroll
+    for (int j = 0; j < PER / 4; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < n; ++k) {
+        const float weight = fast_exp2(stat[at + k * apart][0] - M);
+        l += stat[at + k * apart][1] * weight;
+#pragma unroll
+        for (int j = 0; j < PER / 4; ++j) {
+            const f32x4 o = *reinterpret_cast<const f32x4 *>(&slab[at + k * apart][d + 4 * j]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[j][e] = __builtin_fmaf(o[e], weight, acc[j][e]);
+        }
+    }
+    if (whole) {
+        const float inv = l == 0.f ? 0.f : 1.0f / l;   // (a row that sees nothing is zero)
+        const int row = col / p.g, head = kvh * p.g + col - row * p.g;
+        u32x2 *const op = reinterpret_cast<u32x2 *>(p.out + ((int64_t)(row0 + row) * p.Hq + head) * HD + d);
+#pragma unroll
+        for (int j = 0; j < PER / 4; ++j)
+            op[j] = u32x2{pack2_bf16(acc[j][0] * inv, acc[j][1] * inv), pack2_bf16(acc[j][2] * inv, acc[j][3] * inv)};
+    } else {
+        f32x4 *const ap = reinterpret_cast<f32x4 *>(p.part_acc + part * HD + d);
+#pragma unroll
+        for (int j = 0; j < PER / 4; ++j) ap[j] = acc[j];
+        if (d == 0) *reinterpret_cast<f32x2 *>(p.part_ml + 2 * part) = f32x2{M, l};
+    }
+}
+
 // A wave's share of the loads of a tile of K or of V (one block, one kv head) from the cache into LDS: NL loads of 16 bytes per lane, 1 KiB each,
 // contiguous in LDS from dst on.  off[n]: the lane's place in the tile for load n, less n KiB (the instruction's offset counts for both
 // addresses).  once: nobody else reads the tile, so it need not push anything out of the caches (64 sequences of 16 nodes on 4096 tokens,
@@ -319,7 +377,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_kernel(const TreeArgs p)
     constexpr int64_t kTile = (int64_t)HD * kBlockSize;
     constexpr int kSlab = NW * 32 * ROW * 4, kStage = 2 * 2 * STAGE * 16;
     __shared__ __align__(16) unsigned char lds[kSlab > kStage ? kSlab : kStage];
-    __shared__ float stat[NW][32][2];
+    __shared__ __align__(8) float stat[NW][32][2];
     float (*const slab)[32][ROW] = reinterpret_cast<float (*)[32][ROW]>(lds);           // [wave][column][dim]
     u32x4 *const ldsK = reinterpret_cast<u32x4 *>(lds), *const ldsV = ldsK + 2 * STAGE;   // [buffer][block][piece]
 
@@ -327,21 +385,10 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_kernel(const TreeArgs p)
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, h = lane >> 5;
     const int g = p.g;
-    // Runs next to each other on the line are on one XCD (workgroup b runs on XCD b % 8): the tiles of one sequence and kv head walk the
-    // same tokens at about the same time, and share an L2 (512 columns on 14,000 tokens, us: 286 -> 255).  A line of runs of one
-    // step is spread over the XCDs.
-    int w = blockIdx.x, seq = 0;
+    int w, seq = 0;
     int64_t start = 0;
     TreeSeq s = {};
-    const int64_t total = tree_locate<NT>(
-        p,
-        [&](int64_t t) {
-            const TreeRuns r(p, t);
-            if (r.split && r.log2 >= 3 && w >> r.log2 == 0) w = (w & 7) << (r.log2 - 3) | w >> 3;
-            return r.first(w);
-        },
-        seq, start, s);
-    const TreeRuns runs(p, total);
+    const TreeRuns runs = tree_run<NT>(p, w, seq, start, s);
     const int64_t lo = runs.first(w), hi = runs.first(w + 1);
     int32_t *const merge = p.merges + (int64_t)w * kMergeInts;
     if (lo >= hi) {
@@ -632,45 +679,186 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_kernel(const TreeArgs p)
                 *reinterpret_cast<f32x4 *>(&slab[wave][col][32 * mb + 8 * k + 4 * h]) =
                     f32x4{x.O[mb][4 * k], x.O[mb][4 * k + 1], x.O[mb][4 * k + 2], x.O[mb][4 * k + 3]};
         __syncthreads();
-        constexpr int TC = NT / 32, PER = HD / TC;   // threads of a column, dims of each
         const bool whole = s0 == 0 && s1 == s.steps;
         const int64_t slot = 2 * (int64_t)w + (s0 == 0 ? 1 : 0);   // (a run has one unit that begins before it, and one that ends behind it)
         for (int i = 0; i < waves; ++i) {
-            const int oc = 32 * i + tid / TC, od = (tid % TC) * PER;
-            const int o_row = oc / g, o_head = oc - o_row * g;
-            if (o_row >= rows) break;
-            float M = -INFINITY;
-            for (int k = i; k < NW; k += waves) M = fmaxf(M, stat[k][oc & 31][0]);
-            float l = 0.f;
-            f32x4 acc[PER / 4];
-#pragma unroll
-            for (int j = 0; j < PER / 4; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-            for (int k = i; k < NW; k += waves) {
-                const float weight = fast_exp2(stat[k][oc & 31][0] - M);
-                l += stat[k][oc & 31][1] * weight;
-#pragma unroll
-                for (int j = 0; j < PER / 4; ++j) {
-                    const f32x4 o = *reinterpret_cast<const f32x4 *>(&slab[k][oc & 31][od + 4 * j]);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[j][e] = __builtin_fmaf(o[e], weight, acc[j][e]);
-                }
-            }
-            if (whole) {
-                const float inv = l == 0.f ? 0.f : 1.0f / l;   // (a row that sees nothing is zero)
-                u32x2 *const op = reinterpret_cast<u32x2 *>(p.out + ((int64_t)(s.q0 + row0 + o_row) * p.Hq + kvh * g + o_head) * HD + od);
-#pragma unroll
-                for (int j = 0; j < PER / 4; ++j)
-                    op[j] = u32x2{pack2_bf16(acc[j][0] * inv, acc[j][1] * inv), pack2_bf16(acc[j][2] * inv, acc[j][3] * inv)};
-            } else {
-                f32x4 *const ap = reinterpret_cast<f32x4 *>(p.part_acc + (slot * COLS + oc) * HD + od);
-#pragma unroll
-                for (int j = 0; j < PER / 4; ++j) ap[j] = acc[j];
-                if (tid % TC == 0) {
-                    p.part_ml[(slot * COLS + oc) * 2] = M;
-                    p.part_ml[(slot * COLS + oc) * 2 + 1] = l;
-                }
+            const int oc = 32 * i + tid / (NT / 32);
+            if (oc >= rows * g) break;
+            tree_column<HD, NT, ROW>(p, &slab[0][0], &stat[0][0], 32 * i + (oc & 31), 32 * waves, NW / waves, whole, slot * COLS + oc, s.q0 + row0, oc, kvh);
+        }
+        if (s0 > 0) {   // (at most once, at the beginning of the run)
+            // where all parts of the unit are: the first in the run that the unit begins in, the others at the beginnings of theirs
+            first_run = runs.holding(pos - s0);
+            parts = runs.holding(pos - s0 + s.steps - 1) - first_run + 1;
+            if (tid == 0) {
+                merge[2] = s.q0 + row0;
+                merge[3] = rows;
+                merge[4] = kvh;
             }
         }
+        pos += s1 - s0;
+    }
+    if (tid == 0) {
+        merge[0] = parts;
+        merge[1] = first_run;
+    }
+}
+
+// Tiles of up to 64 columns: every wave has all columns and a quarter of the tokens, whose K and V it loads from the cache to the registers of
+// the matrix instructions.  Two blocks of 32 columns use what is there once; the waves have the registers of a whole SIMD for that, and a
+// turn's loads ahead of the products, 64 KiB of a workgroup, keep the memory busy with one workgroup to a compute unit.
+template <int HD>
+__global__ __launch_bounds__(256, 1) void tree_stream_kernel(const TreeArgs p)
+{
+    constexpr int NW = 4, NT = 64 * NW, COLS = 64;
+    using Wave = TreeWave<HD>;
+    constexpr int KS = Wave::KS, MB = Wave::MB;
+    constexpr int ROW = HD + 4;
+    __shared__ __align__(16) float slab[NW * COLS][ROW];   // [wave, column][dim]
+    __shared__ __align__(8) float stat[NW * COLS][2];
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, h = lane >> 5;
+    const int g = p.g;
+    int w, seq = 0;
+    int64_t start = 0;
+    TreeSeq s = {};
+    const TreeRuns runs = tree_run<NT>(p, w, seq, start, s);
+    const int64_t lo = runs.first(w), hi = runs.first(w + 1);
+    int32_t *const merge = p.merges + (int64_t)w * kMergeInts;
+    if (lo >= hi) {
+        if (tid == 0) merge[0] = 0;
+        return;
+    }
+    const int ku = col >> 4, kslot = (col & 3) | ((col & 4) << 1) | ((col & 8) >> 1);   // (see tree_kernel)
+    const char *const k_cache = reinterpret_cast<const char *>(p.k_cache), *const v_cache = reinterpret_cast<const char *>(p.v_cache);
+    int first_run = 0, parts = 0;
+    for (int64_t pos = lo; pos < hi;) {
+        while (pos - start >= s.units) {
+            start += s.units;
+            ++seq;
+            s = tree_seq_at(p, seq);
+        }
+        const int unit = (int)quotient(pos - start, s.steps);
+        const int s0 = (int)(pos - start - (int64_t)unit * s.steps);
+        const int s1 = (int)min((int64_t)s.steps, s0 + (hi - pos));
+        const int kvh = s.tiles == 1 ? unit : unit / s.tiles, tile = unit - kvh * s.tiles;
+        const int row0 = tile * s.tile_rows, rows = min(s.tile_rows, s.n - row0);
+        const int nblk = (s.len + kBlockSize - 1) / kBlockSize;
+        const const_i32_ptr table = scalar_ptr(p.block_tables + (int64_t)seq * p.max_blocks_per_seq);
+        const int last_id = (int)min(p.num_blocks, (int64_t)INT32_MAX) - 1;
+        auto id_at = [&](int block) -> int { return table[min(block, nblk - 1)]; };   // blocks past the end: the last one
+        auto bytes_at = [&](int id) -> int64_t { return ((int64_t)min(max(id, 0), last_id) * p.Hkv + kvh) * (HD * 32); };
+        // 32 tokens, two blocks, at a time: those of the run from 32 * wave on, every 32 * NW.  Loads behind the wave's last tokens fetch
+        // those again, so that every turn has the same number of loads on their way.
+        const int t_end = min(4 * s1, (s.len + 31) / 32), t0 = 4 * s0 + wave;
+        auto walk = [&](auto blocks) {
+            constexpr int CB = decltype(blocks)::value;   // blocks of 32 columns
+            Wave x[CB];
+#pragma unroll
+            for (int c = 0; c < CB; ++c) {   // (columns behind the last row repeat it)
+                const int at = 32 * c + col, row = min(at / g, rows - 1);
+                x[c].begin(p, (int64_t)s.q0 + row0 + row, kvh * g + at % g, h);
+            }
+            if (t0 < t_end) {
+                const int t_last = t0 + (t_end - 1 - t0) / NW * NW;
+                int ida = id_at(2 * t0), idb = id_at(2 * t0 + 1);
+                u32x4 kr[KS], vr[2][MB];
+                int64_t at0, at1;
+                auto load_k = [&]() {
+                    at0 = bytes_at(ida);
+                    at1 = bytes_at(idb);
+                    const u32x4 *const kp = reinterpret_cast<const u32x4 *>(k_cache + (ku ? at1 : at0));
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks) kr[ks] = __builtin_nontemporal_load(&kp[(2 * ks + h) * kBlockSize + kslot]);
+                };
+                auto load_v = [&]() {
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const u32x4 *const vp = reinterpret_cast<const u32x4 *>(v_cache + (b ? at1 : at0));
+#pragma unroll
+                        for (int mb = 0; mb < MB; ++mb) vr[b][mb] = __builtin_nontemporal_load(&vp[2 * (32 * mb + col) + h]);
+                    }
+                };
+                auto next_ids = [&](int next) {
+                    ida = id_at(2 * min(next, t_last));
+                    idb = id_at(2 * min(next, t_last) + 1);
+                };
+                load_k();
+                __builtin_amdgcn_sched_barrier(kNoVmem);   // (the scores wait for K alone)
+                load_v();
+                next_ids(t0 + NW);
+                for (int t = t0; t < t_end; t += NW) {
+                    const int tok0 = 32 * t, left = s.len - tok0;
+                    f32x16 S[CB];
+#pragma unroll
+                    for (int c = 0; c < CB; ++c)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) S[c][r] = 0.f;
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                        for (int c = 0; c < CB; ++c)
+                            S[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kr[ks]), __builtin_bit_cast(bf16x8, x[c].qb[ks]), S[c], 0, 0, 0);
+                    load_k();
+                    if (left < 32) {
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) {   // (slots past the end may hold anything, and 0 * NaN is NaN)
+                            const int first = 16 * b + 8 * h;
+                            u32x4 keep;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                keep[i] = (first + 2 * i < left ? 0x0000FFFFu : 0u) | (first + 2 * i + 1 < left ? 0xFFFF0000u : 0u);
+#pragma unroll
+                            for (int mb = 0; mb < MB; ++mb) vr[b][mb] &= keep;
+                        }
+                    }
+                    u32x4 P[CB][2];
+#pragma unroll
+                    for (int c = 0; c < CB; ++c) {
+                        x[c].hide(S[c], p.words, tok0, s.ctx, s.len, h);
+                        x[c].add(S[c], P[c]);
+                    }
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+#pragma unroll
+                        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                            for (int c = 0; c < CB; ++c)
+                                x[c].O[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vr[b][mb]), __builtin_bit_cast(bf16x8, P[c][b]),
+                                                                                    x[c].O[mb], 0, 0, 0);
+                    load_v();
+                    next_ids(t + 2 * NW);
+                }
+            }
+            __syncthreads();   // (LDS: the last unit's results have been read)
+#pragma unroll
+            for (int c = 0; c < CB; ++c) {
+                float l0, l1;
+                swap32(x[c].lsum, l0, l1);
+                const int at = wave * COLS + 32 * c + col;
+                if (h == 0) {
+                    stat[at][0] = x[c].m;
+                    stat[at][1] = l0 + l1;
+                }
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        *reinterpret_cast<f32x4 *>(&slab[at][32 * mb + 8 * k + 4 * h]) =
+                            f32x4{x[c].O[mb][4 * k], x[c].O[mb][4 * k + 1], x[c].O[mb][4 * k + 2], x[c].O[mb][4 * k + 3]};
+            }
+        };
+        if (rows * g <= 32)
+            walk(std::integral_constant<int, 1>());
+        else
+            walk(std::integral_constant<int, 2>());
+        __syncthreads();
+        const bool whole = s0 == 0 && s1 == s.steps;
+        const int64_t slot = 2 * (int64_t)w + (s0 == 0 ? 1 : 0);
+        for (int oc = tid / (NT / 32); oc < rows * g; oc += 32)
+            tree_column<HD, NT, ROW>(p, slab, stat, oc, COLS, NW, whole, slot * COLS + oc, s.q0 + row0, oc, kvh);
         if (s0 > 0) {   // (at most once, at the beginning of the run)
             // where all parts of the unit are: the first in the run that the unit begins in, the others at the beginnings of theirs
             first_run = runs.holding(pos - s0);
@@ -762,17 +950,18 @@ hipError_t launch(TreeArgs &a, void *ws, hipStream_t s)
     a.tile_rows = 32 * NW / a.g;
     const int64_t tiles = a.total_q / a.tile_rows + (int64_t)a.num_seqs, steps = (int64_t)a.max_blocks_per_seq * kBlockSize / kTreeStep + 1;
     a.short_line = a.num_seqs <= 64 && (double)tiles * (double)a.Hkv * (double)steps < 2147483647.0;
-    // One workgroup of four waves to a compute unit, and so half the runs, cuts fewer units, but waits with nothing else to do.  With
-    // 32 columns, where its loads are a turn ahead, it is the faster whenever two to a compute unit would have to cut most units (fewer units than runs,
-    // by the average sequence), else on a line of less than four steps a run.  MI355X, us, all runs / half, 32/8 heads: 8 nodes, 8 sequences of 2000 tokens
-    // 27.2 / 22.8, 32 of 4096 98.6 / 90.0, 16 of 20,000 215 / 206, 64 of 100 .. 1000 (as many units as runs) 46.9 / 52.3; 32 sequences of
-    // 32 nodes on 600 tokens (2.5 steps) 45.2 / 32.9, 16 of 24 nodes on 1000 .. 4000 (5) 55.4 / 57.9.
+    // One workgroup of four waves to a compute unit, and so half the runs, cuts fewer units, but waits with nothing else to do: so it is on a
+    // line of less than four steps a run, unless two to a compute unit find whole units.  MI355X, us, all runs / half, 32/8 heads: 32
+    // sequences of 32 nodes on 600 tokens (2.5 steps a run) 45.2 / 32.9, 16 of 24 nodes on 1000 .. 4000 (5) 55.4 / 57.9.
     const int64_t per_seq = ((int64_t)a.total_q + a.num_seqs - 1) / a.num_seqs, units = ((per_seq + a.tile_rows - 1) / a.tile_rows) * a.Hkv * a.num_seqs;
-    a.halve_below = NW == 8 || runs < 2 || units >= (int64_t)runs ? 0 : per_seq * a.g <= 32 ? INT64_MAX : (int64_t)4 << a.runs_log2;
+    a.halve_below = NW != 4 || runs < 2 || units >= (int64_t)runs ? 0 : (int64_t)4 << a.runs_log2;
     a.part_acc = static_cast<float *>(ws);
     a.part_ml = a.part_acc + (size_t)2 * runs * (32 * NW) * HD;
     a.merges = reinterpret_cast<int32_t *>(a.part_ml + (size_t)2 * runs * (32 * NW) * 2);
-    hipLaunchKernelGGL((tree_kernel<HD, NW>), dim3(runs), dim3(64 * NW), 0, s, a);
+    if constexpr (NW == 2)
+        hipLaunchKernelGGL((tree_stream_kernel<HD>), dim3(runs), dim3(256), 0, s, a);
+    else
+        hipLaunchKernelGGL((tree_kernel<HD, NW>), dim3(runs), dim3(64 * NW), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((tree_merge_kernel<HD, NW>), dim3(runs, kMergeSlices), dim3(kMergeThreads), 0, s, a);
@@ -780,7 +969,10 @@ hipError_t launch(TreeArgs &a, void *ws, hipStream_t s)
 }
 }  // namespace
 
-// Workgroups of eight waves fetch K and V once for 256 columns where four waves fetch them twice, at about the same time if the lengths
+// Two: the kernel for up to 64 columns, where the average sequence has no more and there are less than two units for each compute unit, so
+// that two workgroups of the other kernel would have to cut them.  MI355X, us, four waves / this, 32/8 heads: 16 nodes, 32 sequences of 4096 tokens
+// 101.6 / 91.3; 8 nodes, 32 of 4096 98.6 / 88.5, 8 of 2000 27.2 / 22.9; 64 of 100 .. 1000 (two units each) 46.9 / 52.3.
+// Else workgroups of eight waves fetch K and V once for 256 columns where four waves fetch them twice, at about the same time if the lengths
 // are equal and at different times if not; they are fewer, and their waves wait for one another.  So they are for sequences of more
 // than 128 columns on average, and for work that fills them: 16 steps each, of what the block tables can hold (the lengths are on the
 // device).  MI355X, us, four / eight waves, 64 nodes of 32/8 heads: 4 sequences of 1000 tokens 33 / 37, 4 of 4000 43 / 47, 32 of 4096 168 /
@@ -788,19 +980,22 @@ hipError_t launch(TreeArgs &a, void *ws, hipStream_t s)
 int tree_waves(int total_q, int num_seqs, int Hkv, int g, int max_blocks_per_seq, int num_cus)
 {
     const double steps = (double)num_seqs * Hkv * ((double)max_blocks_per_seq * kBlockSize / kTreeStep);
+    const int64_t tile_rows = 64 / g, per_seq = ((int64_t)total_q + num_seqs - 1) / num_seqs;
+    if (per_seq * g <= 64 && (per_seq + tile_rows - 1) / tile_rows * num_seqs * Hkv < 2 * num_cus) return 2;
     return (int64_t)total_q * g > 128 * (int64_t)num_seqs && steps >= 16.0 * num_cus ? 8 : 4;
 }
 
 int tree_runs_log2(int waves, int hd, int num_cus, size_t ws_bytes)
 {
     int log2 = 0;
-    while ((2 << log2) <= 8 / waves * num_cus) ++log2;   // eight waves to a compute unit
+    while ((2 << log2) <= (waves == 4 ? 2 : 1) * num_cus) ++log2;
     while (log2 >= 0 && (run_bytes(hd, waves) << log2) > ws_bytes) --log2;
     return log2;
 }
 
 hipError_t launch_attn_tree(TreeArgs &a, int waves, void *ws, hipStream_t s)
 {
+    if (waves == 2) return a.hd == 128 ? launch<128, 2>(a, ws, s) : launch<64, 2>(a, ws, s);
     if (a.hd == 128) return waves == 8 ? launch<128, 8>(a, ws, s) : launch<128, 4>(a, ws, s);
     return waves == 8 ? launch<64, 8>(a, ws, s) : launch<64, 4>(a, ws, s);
 }
