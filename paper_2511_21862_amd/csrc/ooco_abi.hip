@@ -2186,8 +2186,9 @@ ooco_status ooco_verify_drafts(ooco_ctx *ctx, const void *target_probs, const vo
         return fail(ctx, OOCO_EINVAL, "ooco_verify_drafts: vocab=%d row_stride=%lld max_path=%d", vocab, (long long)row_stride, max_path);
     if (parents && draft_probs) return fail(ctx, OOCO_EINVAL, "ooco_verify_drafts: draft_probs are for chains (parents == NULL)");
     ooco_status st;
-    if (!step_call(ctx, "ooco_verify_drafts", num_seqs, total_q_tokens, st)) return st;
-    if (!target_probs || !tokens || !uniforms || !final_uniforms || !query_start_loc || !counts || (max_path && !path) || !out_tokens)
+    // (a step without rows has counts all the same)
+    if (!step_call(ctx, "ooco_verify_drafts", num_seqs, total_q_tokens == 0 ? 1 : total_q_tokens, st)) return st;
+    if ((total_q_tokens && (!target_probs || !tokens || !uniforms || !final_uniforms)) || !query_start_loc || !counts || (max_path && !path) || !out_tokens)
         return fail(ctx, OOCO_EINVAL, "ooco_verify_drafts: NULL pointer argument");
     if (!aligned(target_probs, bf16_probs ? 2 : 4) || !aligned(draft_probs, bf16_probs ? 2 : 4))
         return fail(ctx, OOCO_EINVAL, "ooco_verify_drafts: probabilities must be aligned to their element");

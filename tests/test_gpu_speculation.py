@@ -451,6 +451,19 @@ def test_verify_rows_apart_and_at_odd_elements():
         assert (g == w).all()
 
 
+def test_verify_of_steps_without_rows():
+    # the counts are the lengths' increments: they are written also where there is no row at all
+    empty = lambda *shape: torch.empty(shape, device="cuda")
+    i32 = lambda *shape: torch.full(shape, 9, dtype=torch.int32, device="cuda")
+    say("case: verification without rows")
+    with B.Context(4, 1, 64, 16, 1, 1) as c:
+        for parents in (i32(0), None):
+            counts, path, out = i32(3), i32(3, 4), i32(3, 5)
+            c.verify_drafts(empty(0, 50), i32(0), empty(0), empty(3), torch.zeros(4, dtype=torch.int32, device="cuda"), counts, path, out, parents=parents)
+            torch.cuda.synchronize()
+            assert (counts == 0).all() and (path == -1).all() and (out == -1).all()
+
+
 def test_verify_borders():
     # nothing left but the row itself, rows without weight, values that are no probabilities, random numbers at their ends
     V = 5000

@@ -158,3 +158,18 @@ def test_both_ways_of_marshalling_give_the_same(monkeypatch):
             assert e.value.status == B.OOCO_EINVAL and "chains" in e.value.message
     for a, b in zip(*results):
         assert (a == b).all()
+
+
+def test_a_step_without_rows_leaves_the_lengths():
+    say("case: step without rows")
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    with B.Context(8, 2, 64, 16, 4, 2) as c:
+        c.rope_set(B.ooco_rope_frequencies("plain", 64)["frequencies"])
+        k, v = (torch.zeros((4, 2) + s, dtype=torch.bfloat16, device="cuda") for s in ((8, 16, 8), (64, 16)))
+        step, lens = TreeStep(c, 16, 4, 8, 64), i32([5, 0, 17])
+        step.begin(i32([]), i32([0, 0, 0, 0]), lens, i32([[0, 1], [2, -1], [3, 0]]))
+        rows = lambda heads: torch.empty((0, heads, 64), dtype=torch.bfloat16, device="cuda")
+        assert step.layer(rows(8), rows(2), rows(2), k, v).shape[0] == 0
+        counts, _ = step.finish(torch.empty((0, 50), device="cuda"), i32([]), torch.empty(0, device="cuda"), torch.rand(3, device="cuda"), [k], [v])
+        torch.cuda.synchronize()
+    assert (counts == 0).all() and lens.tolist() == [5, 0, 17]
