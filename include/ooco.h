@@ -423,7 +423,7 @@ ooco_status ooco_kv_append(ooco_ctx *ctx, const void *k_new /*DEVICE*/, const vo
  * ooco_kv_compact brings their K and V to their places in the caches of all layers.  Node j is token ctx_lens[i] + j of the
  * cache until then.  None of these calls needs a plan or a host copy of a length, none synchronises or copies: they can be
  * recorded into a HIP graph, and a graph replays with the lengths that the device arrays then hold.  Calls are made with
- * the context's device current (-> OOCO_EINVAL).  Sequences of 0 rows, and sequences whose query_start_loc runs outside
+ * the context's device current (-> OOCO_EINVAL).  ctx_lens are not negative.  Sequences of 0 rows, and sequences whose query_start_loc runs outside
  * [0, total_q_tokens], take no part.
  *
  * Masks and positions.  Node t sees node j if j is t or an ancestor of t:

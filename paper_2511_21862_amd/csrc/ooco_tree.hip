@@ -979,7 +979,8 @@ hipError_t launch(TreeArgs &a, void *ws, hipStream_t s)
 {
     const unsigned runs = 1u << a.runs_log2;
     a.tile_rows = 32 * NW / a.g;
-    const int64_t tiles = a.total_q / a.tile_rows + (int64_t)a.num_seqs, steps = (int64_t)a.max_blocks_per_seq * kBlockSize / kTreeStep + 1;
+    // (the bound holds for sequences that overlap as well)
+    const int64_t tiles = (int64_t)a.num_seqs * (a.total_q / a.tile_rows + 1), steps = (int64_t)a.max_blocks_per_seq * kBlockSize / kTreeStep + 1;
     a.short_line = a.num_seqs <= 64 && (double)tiles * (double)a.Hkv * (double)steps < 2147483647.0;
     // One workgroup of four waves to a compute unit, and so half the runs, cuts fewer units, but waits with nothing else to do: so it is on a
     // line of less than four steps a run, unless two to a compute unit find whole units.  MI355X, us, all runs / half, 32/8 heads: 32
