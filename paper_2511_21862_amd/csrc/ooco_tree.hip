@@ -32,7 +32,6 @@ namespace ooco {
 constexpr int kTreeStep = 128;               // tokens of a step
 constexpr int kMaskRow = kMaxMaskWords + 1;  // words of a mask in LDS (padded: the lanes of a wave are columns)
 constexpr int kMergeInts = 5;
-constexpr int kMergeSlices = 8;
 constexpr int kMergeThreads = 256;
 
 // The largest of a lane's sixteen scores, NaN if one is.  (v_maximum3_f32, which needs no operand quieted.  Not the asm of max16:
@@ -908,8 +907,12 @@ __global__ __launch_bounds__(256, 1) void tree_stream_kernel(const TreeArgs p)
     }
 }
 
+// Slices of a run's share of the merge: 16 columns of the widest tile each, at most eight.  (Most workgroups find nothing to do, and take their
+// time: 8 nodes of eight sequences on 2000 tokens, us, eight slices / four 22.9 / 22.0, of one on 300 12.4 / 12.0.)
+constexpr int merge_slices(int waves) { return waves < 4 ? 2 * waves : 8; }
+
 // The parts of the units that runs have cut.  Every run that continues a unit takes a share of its columns, so that a unit of many
-// parts, which has many runs, is merged by many workgroups; kMergeSlices of them have the run's share.  In a workgroup HD / 4 threads
+// parts, which has many runs, is merged by many workgroups; merge_slices of them have the run's share.  In a workgroup HD / 4 threads
 // have a column's dims, and groups of threads have every PG-th part of it; their results meet in LDS in a fixed order.
 template <int HD, int NW>
 __global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(const TreeArgs p)
@@ -922,7 +925,7 @@ __global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(const TreeArg
     const int32_t *const merge = p.merges + (int64_t)w * kMergeInts;
     const int parts = merge[0], first = merge[1], row0 = merge[2], rows = merge[3], kvh = merge[4];
     if (parts == 0) return;
-    const int cols = rows * p.g, shares = (parts - 1) * kMergeSlices, share = (w - first - 1) * kMergeSlices + blockIdx.y;
+    const int cols = rows * p.g, shares = (parts - 1) * merge_slices(NW), share = (w - first - 1) * merge_slices(NW) + blockIdx.y;
     const int c0 = cols * share / shares, c1 = cols * (share + 1) / shares;
     const int groups = parts <= AHEAD ? 1 : parts <= 2 * AHEAD ? 2 : parts <= 4 * AHEAD ? 4 : SLOTS;
     const int slot = threadIdx.x / TC, d = 4 * (threadIdx.x % TC);
@@ -996,7 +999,7 @@ hipError_t launch(TreeArgs &a, void *ws, hipStream_t s)
         hipLaunchKernelGGL((tree_kernel<HD, NW>), dim3(runs), dim3(64 * NW), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((tree_merge_kernel<HD, NW>), dim3(runs, kMergeSlices), dim3(kMergeThreads), 0, s, a);
+    hipLaunchKernelGGL((tree_merge_kernel<HD, NW>), dim3(runs, merge_slices(NW)), dim3(kMergeThreads), 0, s, a);
     return hipGetLastError();
 }
 }  // namespace
