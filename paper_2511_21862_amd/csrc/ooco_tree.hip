@@ -31,6 +31,11 @@ namespace ooco {
 
 constexpr int kTreeStep = 128;               // tokens of a step
 constexpr int kMaskRow = kMaxMaskWords + 1;  // words of a mask in LDS (padded: the lanes of a wave are columns)
+// Steps of the line that a unit has beyond its own, so that a run of many short units is not the last to end: the first loads, which nothing
+// hides, and the end of a unit take about as long.  Not on lines of less than four steps a run, whose runs begin and end one unit anyway.
+// (MI355X, us, 0 / 1 / 2 / 4 of them: 32 sequences of 5 .. 16 nodes on 512 .. 8192 tokens, 32/8 heads 113.5 / 107.7 / 103.4 / 102.7, of 64 nodes
+// 194 / 184 / 181 / 179, 64 of 16 nodes 217 / 213 / 212 / 218.)
+constexpr int kUnitSteps = 2;
 constexpr int kMergeInts = 5;
 constexpr int kMergeThreads = 256;
 
@@ -47,11 +52,12 @@ OOCO_DEV float largest(const f32x16 &s)
 // What a sequence has on the line.
 struct TreeSeq {
     int q0, n, ctx, len, steps;      // len: tokens that exist, the nodes among them
+    int length;                      // of a unit on the line: its steps, and what its beginning and end take
     int tile_rows, tiles;            // rows of a tile but the last
     int last_waves;                  // waves that have columns of the last tile: 1, 2, 4 or 8
     int64_t units;                   // steps of all its units
 };
-OOCO_DEV TreeSeq tree_seq(const TreeArgs &p, int q0, int q1, int ctx)
+OOCO_DEV TreeSeq tree_seq(const TreeArgs &p, int q0, int q1, int ctx, int pad)
 {
     TreeSeq s;
     s.q0 = q0;
@@ -61,11 +67,12 @@ OOCO_DEV TreeSeq tree_seq(const TreeArgs &p, int q0, int q1, int ctx)
     s.ctx = min(max(ctx, 0), cap);
     s.len = (int)min((int64_t)s.ctx + min(s.n, 64 * p.words), (int64_t)cap);
     s.steps = (s.len + kTreeStep - 1) / kTreeStep;
+    s.length = s.steps + pad;
     s.tile_rows = p.tile_rows;       // (a group of heads that does not divide a tile: the columns behind the last whole row are none)
     s.tiles = (s.n + s.tile_rows - 1) / s.tile_rows;
     const int last_cols = (s.n - (s.tiles - 1) * s.tile_rows) * p.g;
     s.last_waves = last_cols <= 32 ? 1 : last_cols <= 64 ? 2 : last_cols <= 128 ? 4 : 8;
-    s.units = (int64_t)s.tiles * p.Hkv * s.steps;
+    s.units = (int64_t)s.tiles * p.Hkv * s.length;
     return s;
 }
 // floor(a / b) of numbers below 2^53: a correctly rounded quotient does not reach the next integer.  (The compiler's 64-bit division
@@ -81,10 +88,10 @@ OOCO_DEV int64_t uniform(int64_t v)
 // Lengths and block ids by scalar loads, which the waits on the vector-memory counter do not see.
 typedef const __attribute__((address_space(4))) int32_t *const_i32_ptr;
 OOCO_DEV const_i32_ptr scalar_ptr(const int32_t *p) { return (const_i32_ptr)(uintptr_t)p; }
-OOCO_DEV TreeSeq tree_seq_at(const TreeArgs &p, int seq)
+OOCO_DEV TreeSeq tree_seq_at(const TreeArgs &p, int seq, int pad)
 {
     const const_i32_ptr qsl = scalar_ptr(p.query_start_loc), ctx = scalar_ptr(p.ctx_lens);
-    return tree_seq(p, qsl[seq], qsl[seq + 1], ctx[seq]);
+    return tree_seq(p, qsl[seq], qsl[seq + 1], ctx[seq], pad);
 }
 
 // Runs of the line: run w = [first(w), first(w + 1)).  No run is empty but those behind the last.  As many as there are workgroups, or half as
@@ -110,26 +117,35 @@ OOCO_DEV int64_t tree_locate(const TreeArgs &p, At at, int &seq, int64_t &start,
     if (p.short_line) {
         const int i = threadIdx.x & 63, j = min(i, p.num_seqs - 1);
         const int q0 = p.query_start_loc[j], q1 = p.query_start_loc[j + 1], ctx = p.ctx_lens[j];
-        const int units = i < p.num_seqs ? (int)tree_seq(p, q0, q1, ctx).units : 0;
-        int incl = units;
+        const TreeSeq own = tree_seq(p, q0, q1, ctx, 0);
+        auto scan = [&](int v) -> int {
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int o = __shfl_up(incl, d);
-            incl += i >= d ? o : 0;
+            for (int d = 1; d < 64; d <<= 1) {
+                const int o = __shfl_up(v, d);
+                v += i >= d ? o : 0;
+            }
+            return v;
+        };
+        int units = i < p.num_seqs ? (int)own.units : 0, incl = scan(units), total = __builtin_amdgcn_readlane(incl, 63), pad = 0;
+        if (total >= (int64_t)4 << p.runs_log2) {
+            pad = kUnitSteps;
+            units += i < p.num_seqs ? own.tiles * p.Hkv * pad : 0;
+            incl = scan(units);
+            total = __builtin_amdgcn_readlane(incl, 63);
         }
-        const int total = __builtin_amdgcn_readlane(incl, 63);
         const int64_t x = at((int64_t)total);
         seq = min(__popcll(__ballot(incl <= x)), p.num_seqs - 1);
         start = __builtin_amdgcn_readlane(incl - units, seq);
-        found = tree_seq(p, __builtin_amdgcn_readlane(q0, seq), __builtin_amdgcn_readlane(q1, seq), __builtin_amdgcn_readlane(ctx, seq));
+        found = tree_seq(p, __builtin_amdgcn_readlane(q0, seq), __builtin_amdgcn_readlane(q1, seq), __builtin_amdgcn_readlane(ctx, seq), pad);
         return total;
     }
     __shared__ int64_t wave_total[NT / 64];
     __shared__ int sh_seq;
     __shared__ int64_t sh_start;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int pad = 0;
     auto units_of = [&](int i) -> int64_t {
-        return i < p.num_seqs ? tree_seq(p, p.query_start_loc[i], p.query_start_loc[i + 1], p.ctx_lens[i]).units : 0;
+        return i < p.num_seqs ? tree_seq(p, p.query_start_loc[i], p.query_start_loc[i + 1], p.ctx_lens[i], pad).units : 0;
     };
     auto scan = [&](int64_t v, int64_t &all) -> int64_t {   // inclusive sum over the workgroup, and of all
         int64_t x = v;
@@ -151,10 +167,18 @@ OOCO_DEV int64_t tree_locate(const TreeArgs &p, At at, int &seq, int64_t &start,
         return before + x;
     };
     int64_t total = 0, all, mine = 0, incl = 0;
-    for (int base = 0; base < p.num_seqs; base += NT) {
-        mine = units_of(base + tid);
-        incl = scan(mine, all);
-        total += all;
+    auto measure = [&]() {
+        total = 0;
+        for (int base = 0; base < p.num_seqs; base += NT) {
+            mine = units_of(base + tid);
+            incl = scan(mine, all);
+            total += all;
+        }
+    };
+    measure();
+    if (total >= (int64_t)4 << p.runs_log2) {   // (the same in every thread)
+        pad = kUnitSteps;
+        measure();
     }
     const int64_t x = at(total);
     int64_t before = 0;
@@ -176,7 +200,7 @@ OOCO_DEV int64_t tree_locate(const TreeArgs &p, At at, int &seq, int64_t &start,
     if (x >= total) return uniform(total);
     seq = __builtin_amdgcn_readfirstlane(sh_seq);
     start = uniform(sh_start);
-    found = tree_seq_at(p, seq);
+    found = tree_seq_at(p, seq, pad);
     return uniform(total);
 }
 
@@ -445,10 +469,14 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_kernel(const TreeArgs p)
         while (pos - start >= s.units) {   // the next sequence with rows
             start += s.units;
             ++seq;
-            s = tree_seq_at(p, seq);
+            s = tree_seq_at(p, seq, s.length - s.steps);
         }
-        const int unit = (int)quotient(pos - start, s.steps);
-        const int s0 = (int)(pos - start - (int64_t)unit * s.steps);
+        const int unit = (int)quotient(pos - start, s.length);
+        const int s0 = (int)(pos - start - (int64_t)unit * s.length);
+        if (s0 >= s.steps) {
+            pos += s.length - s0;
+            continue;
+        }
         const int s1 = (int)min((int64_t)s.steps, s0 + (hi - pos));
         const int kvh = s.tiles == 1 ? unit : unit / s.tiles, tile = unit - kvh * s.tiles;
         const int waves = tile == s.tiles - 1 ? s.last_waves : NW;
@@ -768,10 +796,14 @@ __global__ __launch_bounds__(256, 1) void tree_stream_kernel(const TreeArgs p)
         while (pos - start >= s.units) {
             start += s.units;
             ++seq;
-            s = tree_seq_at(p, seq);
+            s = tree_seq_at(p, seq, s.length - s.steps);
         }
-        const int unit = (int)quotient(pos - start, s.steps);
-        const int s0 = (int)(pos - start - (int64_t)unit * s.steps);
+        const int unit = (int)quotient(pos - start, s.length);
+        const int s0 = (int)(pos - start - (int64_t)unit * s.length);
+        if (s0 >= s.steps) {
+            pos += s.length - s0;
+            continue;
+        }
         const int s1 = (int)min((int64_t)s.steps, s0 + (hi - pos));
         const int kvh = s.tiles == 1 ? unit : unit / s.tiles, tile = unit - kvh * s.tiles;
         const int row0 = tile * s.tile_rows, rows = min(s.tile_rows, s.n - row0);
@@ -983,7 +1015,7 @@ hipError_t launch(TreeArgs &a, void *ws, hipStream_t s)
     const unsigned runs = 1u << a.runs_log2;
     a.tile_rows = 32 * NW / a.g;
     // (the bound holds for sequences that overlap as well)
-    const int64_t tiles = (int64_t)a.num_seqs * (a.total_q / a.tile_rows + 1), steps = (int64_t)a.max_blocks_per_seq * kBlockSize / kTreeStep + 1;
+    const int64_t tiles = (int64_t)a.num_seqs * (a.total_q / a.tile_rows + 1), steps = (int64_t)a.max_blocks_per_seq * kBlockSize / kTreeStep + 1 + kUnitSteps;
     a.short_line = a.num_seqs <= 64 && (double)tiles * (double)a.Hkv * (double)steps < 2147483647.0;
     // One workgroup of four waves to a compute unit, and so half the runs, cuts fewer units, but waits with nothing else to do: so it is on a
     // line of less than four steps a run, unless two to a compute unit find whole units.  MI355X, us, all runs / half, 32/8 heads: 32
