@@ -224,10 +224,11 @@ OOCO_DEV TreeRuns tree_run(const TreeArgs &p, int &w, int &seq, int64_t &start, 
 }
 
 // What a wave does with 32 tokens, whichever way they come: its 32 query columns' share of the softmax and of the output.
-// KEPT: masks are read from LDS.  A load from where they lie would wait for the K and V ahead of it, at every 32 nodes (20 .. 27 nodes of 28/4 heads on
-// 60..131K tokens, 4 sequences, us: 226 -> 208; 64 nodes of 32/8 on 4096, 64 sequences: 322 -> 307).  The small trees of tree_stream_kernel
-// have few such loads, and are the slower for the way through LDS (5 .. 16 nodes on 512 .. 8192, 32 sequences, us: 113.5 / 115.9).
-template <int HD, bool KEPT>
+// KEPT: masks are read from LDS, where K and V are too.  A load from where they lie would wait for the K and V ahead of it, at every 32 nodes (20
+// .. 27 nodes of 28/4 heads on 60..131K tokens, 4 sequences, us: 226 -> 208; 64 nodes of 32/8 on 4096, 64 sequences: 322 -> 307).  Small trees
+// whose K and V go to registers have few such loads, and are the slower for the way through LDS (8 nodes on 300, 128 sequences, us: 41.5 /
+// 46.0; 5 .. 16 on 512 .. 8192, 32 sequences: 113.5 / 115.9).
+template <int HD>
 struct TreeWave {
     static constexpr int KS = HD / 16;   // k-steps of QK
     static constexpr int MB = HD / 32;   // 32-dim groups of the output
@@ -235,9 +236,7 @@ struct TreeWave {
     f32x16 O[MB];
     float m, lsum;                       // reference of the column's weights in log2 units, this lane's share of their sum
     float scale;                         // of scores, to log2 units
-    const uint64_t *mask;
-    int words;                           // that the mask has
-    uint64_t sent[kMaxMaskWords / 2];    // KEPT: this lane's half of it, on its way to LDS
+    const uint64_t *mask;                // the column's; in LDS after keep_mask
 
     OOCO_DEV void begin(const TreeArgs &p, int64_t q_row, int head, int h)
     {
@@ -245,14 +244,6 @@ struct TreeWave {
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) qb[ks] = qp[2 * ks + h];
         mask = p.masks + q_row * p.words;
-        words = p.words;
-        if constexpr (KEPT) {
-#pragma unroll
-            for (int i = 0; i < kMaxMaskWords / 2; ++i) {
-                const int k = kMaxMaskWords / 2 * h + i;
-                sent[i] = k < words ? mask[k] : 0;
-            }
-        }
         scale = p.scale_log2e;
         none();
     }
@@ -265,25 +256,27 @@ struct TreeWave {
         m = -1e30f;   // (finite: tokens that a column does not see weigh nothing, where -inf - -inf would make them NaN)
         lsum = 0.f;
     }
-    // After begin, and before any hide.
-    OOCO_DEV void keep_mask(uint64_t (&row)[kMaskRow], int h)
+    // The mask to LDS, for hide<true>; words behind the mask's own are zero.
+    OOCO_DEV void keep_mask(uint64_t (&row)[kMaskRow], int words, int h)
     {
-        static_assert(KEPT, "masks in LDS");
 #pragma unroll
-        for (int i = 0; i < kMaxMaskWords / 2; ++i) row[kMaxMaskWords / 2 * h + i] = sent[i];
+        for (int i = 0; i < kMaxMaskWords / 2; ++i) {
+            const int k = kMaxMaskWords / 2 * h + i;
+            row[k] = k < words ? mask[k] : 0;
+        }
         mask = row;
-        words = kMaxMaskWords;   // (those behind the mask's own are zero)
     }
     // Hides the scores of tokens that the column does not see.  Register r of S is token tok0 + 16 (r / 8) + 8 h + r % 8.
-    OOCO_DEV void hide(f32x16 &S, int tok0, int ctx, int len, int h) const
+    template <bool KEPT>
+    OOCO_DEV void hide(f32x16 &S, int words, int tok0, int ctx, int len, int h) const
     {
         const int j0 = tok0 - ctx;   // node that token tok0 is (negative: cached)
         if (j0 <= -32) return;
         uint32_t bits;               // bit i: the column sees token tok0 + i
         if (j0 >= 0) {
             const int k = j0 >> 6, sh = j0 & 63;
-            uint64_t b = k < words ? mask[k] >> sh : 0;
-            if (sh > 32 && k + 1 < words) b |= mask[k + 1] << (64 - sh);
+            uint64_t b = k < (KEPT ? kMaxMaskWords : words) ? mask[k] >> sh : 0;
+            if (sh > 32 && k + 1 < (KEPT ? kMaxMaskWords : words)) b |= mask[k + 1] << (64 - sh);
             bits = (uint32_t)b;
         } else {
             bits = ((uint32_t)mask[0] << -j0) | ((1u << -j0) - 1u);
@@ -419,7 +412,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_kernel(const TreeArgs p)
     constexpr int NT = 64 * NW, COLS = 32 * NW;
     constexpr int SHARE = NW / kStageBlocks;      // waves that bring a block
     constexpr int NL = HD / 32 / SHARE;           // loads of a wave for its share of a tile
-    using Wave = TreeWave<HD, true>;
+    using Wave = TreeWave<HD>;
     constexpr int KS = Wave::KS, MB = Wave::MB;
     constexpr int ROW = HD + 4;                   // floats of a column in LDS (padded: the lanes of a wave are columns)
     constexpr int CH = 2 * HD;                    // 16-byte pieces of a tile of K or V
@@ -528,7 +521,6 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_kernel(const TreeArgs p)
                 load_k();
                 __builtin_amdgcn_sched_barrier(kNoVmem);   // (the scores wait for K alone)
                 load_v();
-                x.keep_mask(masks[wave][col], h);
                 next_ids(t + NW);
                 for (; t < t_end; t += NW) {
                     const int tok0 = 32 * t, left = s.len - tok0;
@@ -539,7 +531,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_kernel(const TreeArgs p)
                     for (int ks = 0; ks < KS; ++ks)
                         S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kr[ks]), __builtin_bit_cast(bf16x8, x.qb[ks]), S, 0, 0, 0);
                     load_k();
-                    x.hide(S, tok0, s.ctx, s.len, h);
+                    x.template hide<false>(S, p.words, tok0, s.ctx, s.len, h);
                     if (left < 32) {
 #pragma unroll
                         for (int b = 0; b < 2; ++b) {   // (slots past the end may hold anything, and 0 * NaN is NaN)
@@ -600,7 +592,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_kernel(const TreeArgs p)
             stage_v(f0, id0);
             if (waves < NW) {
                 x.begin(p, q_row, kvh * g + c_head, h);
-                x.keep_mask(masks[wave][col], h);
+                x.keep_mask(masks[wave][col], p.words, h);
                 for (int f = f0; f < f1; ++f) {   // half a stage for each of two waves that have the same columns
                     arrive(f);
                     if (f + 1 < f1) {
@@ -615,7 +607,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_kernel(const TreeArgs p)
 #pragma unroll
                     for (int ks = 0; ks < KS; ++ks)
                         S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k_operand(f, kw, ks)), __builtin_bit_cast(bf16x8, x.qb[ks]), S, 0, 0, 0);
-                    x.hide(S, kStageTokens * f + 32 * kw, s.ctx, s.len, h);
+                    x.template hide<true>(S, p.words, kStageTokens * f + 32 * kw, s.ctx, s.len, h);
                     u32x4 P[2];
                     x.add(S, P);
 #pragma unroll
@@ -628,7 +620,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_kernel(const TreeArgs p)
                 // of the half after next while the vector ALU turns the scores of the half between them into weights.  K runs a stage ahead of V.
                 if (f0 + 1 < f1) stage_k(f0 + 1, id1);
                 x.begin(p, q_row, kvh * g + c_head, h);
-                x.keep_mask(masks[wave][col], h);
+                x.keep_mask(masks[wave][col], p.words, h);
                 int id2 = stage_id(f0 + 2);
                 constexpr int AHEAD = 2;   // products ahead of which an operand is asked for
                 u32x4 ring[AHEAD];
@@ -690,7 +682,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_kernel(const TreeArgs p)
                     }
                     x.lsum += sum;
                 };
-                auto hide = [&](f32x16 &S, int f, int half) { x.hide(S, kStageTokens * f + 32 * half, s.ctx, s.len, h); };
+                auto hide = [&](f32x16 &S, int f, int half) { x.template hide<true>(S, p.words, kStageTokens * f + 32 * half, s.ctx, s.len, h); };
                 f32x16 S0 = {}, S1 = {};
                 u32x4 P0[2] = {}, P1[2] = {};
                 arrive(f0);
@@ -769,7 +761,7 @@ template <int HD>
 __global__ __launch_bounds__(256, 1) void tree_stream_kernel(const TreeArgs p)
 {
     constexpr int NW = 4, NT = 64 * NW, COLS = 64;
-    using Wave = TreeWave<HD, false>;
+    using Wave = TreeWave<HD>;
     constexpr int KS = Wave::KS, MB = Wave::MB;
     constexpr int ROW = HD + 4;
     __shared__ __align__(16) float slab[NW * COLS][ROW];   // [wave, column][dim]
@@ -879,7 +871,7 @@ __global__ __launch_bounds__(256, 1) void tree_stream_kernel(const TreeArgs p)
                     u32x4 P[CB][2];
 #pragma unroll
                     for (int c = 0; c < CB; ++c) {
-                        x[c].hide(S[c], tok0, s.ctx, s.len, h);
+                        x[c].template hide<false>(S[c], p.words, tok0, s.ctx, s.len, h);
                         x[c].add(S[c], P[c]);
                     }
 #pragma unroll
