@@ -19,7 +19,7 @@
 // What bounds it, on MI355X: memory for small trees (32 sequences of 8 nodes of 32/8 heads on 4096 tokens: 88.5 us, 6.1 TB/s; a large copy
 // moves 5.2); for wide ones the matrix cores and the LDS ports that feed them, each busy half of the cycles at 1.9 GHz (8 sequences of 64
 // nodes of 64/8 heads on 14,000: 248 us, 945 TFLOP/s of the 1226 that a large product of matrices reaches); the chain lengths - block ids -
-// tiles - merge for one small sequence (8 nodes on 700 tokens: 10.7 us).
+// tiles - merge for one small sequence (8 nodes on 700 tokens: 10.2 us).
 #include "ooco_device.h"
 #include "ooco_internal.h"
 #include "ooco_spec.h"
